@@ -330,6 +330,87 @@ adept_status adept_attend(adept_dtype dt, int n_heads, int head_dim, float scale
                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Paged caches.  One layer's K and V as n_pages pages of page_size token slots:
+ * slot = page * page_size + offset, so a cache of this kind has the layout
+ * [n_slots][Hkv][hd] that adept_layer_step and adept_kv_generate write through
+ * `slot`, and only the order of a sequence's slots is free: token t of sequence
+ * b sits in page page_table[b][t / page_size] at offset t % page_size.
+ *
+ * Element types: float, bfloat16, or FP8: OCP e4m3 codes with one scale byte per
+ * (slot, head) row of K and of V, 127 + E for the scale 2^E.  A row is
+ * quantised to the least power of two with which its largest finite magnitude
+ * is at most 448 (e4m3's largest), within 2^-100 .. 2^100; every value is then
+ * divided by it (exactly), rounded to the nearest code (ties to even) and, where
+ * the bound 2^100 was met, saturated; infinities and NaN become the NaN code.
+ * e4m3 is a floating format: a scale between two powers of two would not make
+ * its relative error smaller, and with these the codes of a row are defined to
+ * the bit.  Reading back is exact in either source type (4 significant bits).
+ *
+ * page_size is a power of two (1 .. 1024), head_dim a power of two (16 .. 256),
+ * n_pages * page_size below 2^31; k, v and the scales 16-byte aligned.  A call
+ * takes at most 2^23 rows or entries.
+ * ------------------------------------------------------------------------- */
+typedef enum { ADEPT_KV_F32 = 0, ADEPT_KV_BF16 = 1, ADEPT_KV_FP8 = 2 } adept_kv_dtype;
+
+typedef struct {       /* (host); the pointers are device pointers */
+  int32_t dtype;       /* adept_kv_dtype */
+  int32_t n_kv_heads, head_dim;
+  int32_t page_size, n_pages;
+  void* k;             /* [n_pages*page_size][Hkv][hd] */
+  void* v;
+  uint8_t* k_scale;    /* FP8: [n_pages*page_size][Hkv]; else unused */
+  uint8_t* v_scale;
+} adept_paged_kv;
+
+/* Writes K/V rows into their slots: for i < *n_rows (<= max_rows; n_rows NULL:
+ * exactly max_rows), j = rows ? rows[i] : i, row j of k and v ([.][Hkv][hd] of
+ * type dt, rows k_stride / v_stride elements apart, heads contiguous) goes to
+ * slot[j].  The cache's type is dt's or FP8.  A slot outside the cache is
+ * skipped (-1: no place).  The listed slots are distinct; rows not listed are
+ * left as they were.  k, v 16-byte aligned, strides multiples of 16 bytes. */
+adept_status adept_paged_store(adept_dtype dt, const adept_paged_kv* kv, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride,
+                               const int32_t* rows, const int32_t* n_rows, int max_rows,
+                               const int32_t* slot, void* stream);
+
+/* Reads rows back: for i < *n_rows (as above), k[i] and v[i] (type dt, rows
+ * k_stride / v_stride elements apart) = the values the cache holds at slot[i];
+ * zeros for a slot outside the cache.  Later rows are left as they were. */
+adept_status adept_paged_load(adept_dtype dt, const adept_paged_kv* kv, const int32_t* slot,
+                              const int32_t* n_rows, int max_rows, void* k, int64_t k_stride,
+                              void* v, int64_t v_stride, void* stream);
+
+/* adept_attend over a paged cache: new tokens (one per sequence, or a chunk of
+ * a prompt) attend over the tokens before them and, causally, over each other.
+ *
+ *  q [max_active][H][hd] (dt: float over an F32 or FP8 cache, bfloat16 over a
+ *  BF16 or FP8 one), compacted as for adept_attend; H a multiple of Hkv, query
+ *  head h reads K/V head h / (H / Hkv).
+ *  rows[k], k < *n_active (<= max_active); pos, seq by row, in any order
+ *  (a sequence's rows next to each other share what they read).
+ *  causal=1: entry k attends to tokens 0 .. pos[row], below key_len[seq] where
+ *  key_len is given (nullable); causal=0: to tokens 0 .. key_len[seq]-1.
+ *  page_table [n_seq][max_pages] int32: a page outside 0 .. n_pages-1 holds no
+ *  keys; nothing behind max_pages * page_size tokens is seen (a product below
+ *  2^31).  Entries that no query reaches are not read as pages.
+ *  key_live [n_pages*page_size] uint8, by slot, nullable: slots with 0 are
+ *  left out.
+ *  out [max_active][H][hd] (dt): softmax(q K^T * scale) V per head, scores and
+ *  sums in f32; zeros for an entry that sees no key (or whose sequence is
+ *  outside 0 .. n_seq-1).  What is left out has no influence, whatever it holds.
+ *  Entries behind the last active one are left as they were.
+ *  workspace: adept_paged_attend_workspace_bytes() bytes, 16-byte aligned; its
+ *  contents on entry do not matter.  Calls that may overlap need their own. */
+size_t adept_paged_attend_workspace_bytes(const adept_paged_kv* kv, int n_heads, int max_active,
+                                          int n_seq, int max_pages);
+adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv* kv, int n_heads, float scale,
+                                int causal, const void* q, const int32_t* rows,
+                                const int32_t* n_active, int max_active, const int32_t* pos,
+                                const int32_t* seq, int n_seq, const int32_t* page_table,
+                                int max_pages, const int32_t* key_len, const uint8_t* key_live,
+                                void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Whole-layer orchestration of the generative path (Appendix I):
  * adept_layer_step(layer=i) enqueues, for the rows of active[(i-1)&1]
  * (LLAMA family; GPT2: LayerNorm for the norms, biased projections without

@@ -16,6 +16,7 @@ import torch
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libadept.so")
 
 F32, BF16 = 0, 1
+KV_F32, KV_BF16, KV_FP8 = 0, 1, 2
 FAMILY_LLAMA, FAMILY_GPT2 = 0, 1
 SIM_GLOBAL, SIM_LOCAL, SIM_BOTH = 0, 1, 2
 METRICS = {"global": SIM_GLOBAL, "local": SIM_LOCAL, "both": SIM_BOTH}
@@ -78,6 +79,11 @@ class EncoderArgs(ctypes.Structure):
     ]
 
 
+class PagedKv(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("page_size", _i32),
+                ("n_pages", _i32), ("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp)]
+
+
 _SIGS = {
     "adept_abi_version": (_i32, []),
     "adept_last_error": (ctypes.c_char_p, []),
@@ -110,6 +116,14 @@ _SIGS = {
     "adept_attend_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32, _i32]),
     "adept_attend": (_i32, [_i32, _i32, _i32, ctypes.c_float, _i32, _vp, _vp, _vp, _i32, _vp,
                             _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "adept_paged_store": (_i32, [_i32, ctypes.POINTER(PagedKv), _vp, _i64, _vp, _i64, _vp, _vp,
+                                 _i32, _vp, _vp]),
+    "adept_paged_load": (_i32, [_i32, ctypes.POINTER(PagedKv), _vp, _vp, _i32, _vp, _i64, _vp,
+                                _i64, _vp]),
+    "adept_paged_attend_workspace_bytes": (_sz, [ctypes.POINTER(PagedKv), _i32, _i32, _i32, _i32]),
+    "adept_paged_attend": (_i32, [_i32, ctypes.POINTER(PagedKv), _i32, ctypes.c_float, _i32, _vp,
+                                  _vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp,
+                                  _sz, _vp]),
     "adept_layer_workspace_bytes": (_sz, [ctypes.POINTER(LayerArgs)]),
     "adept_layer_step": (_i32, [ctypes.POINTER(LayerArgs), _i32, _vp]),
     "adept_embed": (_i32, [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
@@ -342,6 +356,124 @@ def attend(n_heads, head_dim, q, rows, n_active, max_active, pos, seq, n_seq, k_
                               ptr(k_layer), ptr(v_layer), s_max, ptr(key_len), ptr(key_live),
                               ptr(out), ptr(workspace), ws_bytes, stream_handle(stream)),
            "adept_attend")
+
+
+_KV_TYPES = {torch.float32: KV_F32, torch.bfloat16: KV_BF16, torch.uint8: KV_FP8,
+             torch.float8_e4m3fn: KV_FP8}
+
+
+def _need(cond, what):
+    if not cond:
+        raise AdeptError(what)
+
+
+def _need_here(what, *tensors):
+    """Tensors on the current device (the library launches on its streams)."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        _need(t is None or (t.is_cuda and t.device.index == here),
+              f"{what}: tensors must be on the current HIP device")
+
+
+def _need_i32(what, *tensors):
+    for t in tensors:
+        _need(t is None or (t.dtype == torch.int32 and t.is_contiguous()),
+              f"{what}: index tensors must be contiguous int32")
+
+
+def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
+    """Descriptor of one layer's paged cache: k, v [n_slots, Hkv, hd] (f32, bf16, or e4m3 codes as
+    uint8 / float8_e4m3fn with k_scale, v_scale uint8 [n_slots, Hkv]), contiguous, n_slots a
+    multiple of page_size.  It holds the tensors."""
+    _need(k.dim() == 3 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in _KV_TYPES and
+          k.is_contiguous() and v.is_contiguous(),
+          "paged_kv: k and v must be contiguous [n_slots, Hkv, hd] of one cache type")
+    _need(page_size >= 1 and k.shape[0] % page_size == 0,
+          f"paged_kv: {k.shape[0]} slots are no multiple of the page size {page_size}")
+    fp8 = _KV_TYPES[k.dtype] == KV_FP8
+    _need(fp8 == (k_scale is not None) == (v_scale is not None),
+          "paged_kv: scales go with an 8-bit cache, and only with it")
+    for s in (k_scale, v_scale) if fp8 else ():
+        _need(s.dtype == torch.uint8 and s.shape == k.shape[:2] and s.is_contiguous(),
+              "paged_kv: scales must be contiguous uint8 [n_slots, Hkv]")
+    kv = PagedKv(_KV_TYPES[k.dtype], k.shape[1], k.shape[2], page_size, k.shape[0] // page_size,
+                 ptr(k), ptr(v), ptr(k_scale), ptr(v_scale))
+    kv.tensors = (k, v, k_scale, v_scale)
+    return kv
+
+
+def _paged_rows(what, kv, k, v):
+    _need_here(what, *kv.tensors)
+    dims = (kv.n_kv_heads, kv.head_dim)
+    for t in (k, v):
+        _need(t.dim() == 3 and tuple(t.shape[1:]) == dims and t.dtype == k.dtype and
+              t.dtype in (torch.float32, torch.bfloat16) and
+              (t.shape[0] == 0 or (t.stride(2) == 1 and t.stride(1) == dims[1])),
+              f"{what}: rows must be f32 or bf16 [n, {dims[0]}, {dims[1]}] with contiguous heads")
+
+
+def _row_stride(t):
+    """Elements between the rows of [n, H, hd] (of one row or none: any)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def paged_store(kv, k, v, slot, rows=None, n_rows=None, stream=None):
+    """Rows of k, v [n, Hkv, hd] (any row stride) into the slots slot[row] of the cache, quantised
+    if it is an 8-bit one; rows: the listed rows only, n_rows (device int32 [1]): how many of
+    them."""
+    _paged_rows("paged_store", kv, k, v)
+    _need_here("paged_store", k, v, slot, rows, n_rows)
+    _need_i32("paged_store", slot, rows, n_rows)
+    _need(k.shape[0] == v.shape[0] == slot.numel(), "paged_store: one slot for each row")
+    n = k.shape[0] if rows is None else rows.numel()
+    _check(lib().adept_paged_store(dtype_code(k), ctypes.byref(kv), ptr(k), _row_stride(k), ptr(v),
+                                   _row_stride(v), ptr(rows), ptr(n_rows), n, ptr(slot),
+                                   stream_handle(stream)), "adept_paged_store")
+
+
+def paged_load(kv, slot, k, v, n_rows=None, stream=None):
+    """k[i], v[i] = the cache's values at slot[i] (k, v [n, Hkv, hd], any row stride)."""
+    _paged_rows("paged_load", kv, k, v)
+    _need_here("paged_load", k, v, slot, n_rows)
+    _need_i32("paged_load", slot, n_rows)
+    n = slot.numel()
+    _need(k.shape[0] >= n and v.shape[0] >= n, "paged_load: fewer output rows than slots")
+    _check(lib().adept_paged_load(dtype_code(k), ctypes.byref(kv), ptr(slot), ptr(n_rows), n, ptr(k),
+                                  _row_stride(k), ptr(v), _row_stride(v), stream_handle(stream)),
+           "adept_paged_load")
+
+
+def paged_attend_workspace_bytes(kv, n_heads, max_active, n_seq, max_pages):
+    return lib().adept_paged_attend_workspace_bytes(ctypes.byref(kv), n_heads, max_active, n_seq,
+                                                    max_pages)
+
+
+def paged_attend(kv, q, rows, n_active, max_active, pos, seq, n_seq, page_table, out, causal=True,
+                 key_len=None, key_live=None, workspace=None, scale=None, stream=None):
+    """Attention of the entries q [max_active, H, hd] over the paged cache kv; page_table int32
+    [n_seq, max_pages].  workspace: uint8, paged_attend_workspace_bytes()."""
+    H, hd = q.shape[1], q.shape[2]
+    _need_here("paged_attend", *kv.tensors, q, rows, n_active, pos, seq, page_table, out, key_len,
+               key_live, workspace)
+    _need_i32("paged_attend", rows, n_active, pos, seq, page_table, key_len)
+    _need(q.is_contiguous() and out.is_contiguous() and out.dtype == q.dtype and
+          q.dtype in (torch.float32, torch.bfloat16) and hd == kv.head_dim and
+          q.shape[0] >= max_active and out.numel() >= max_active * H * hd and
+          rows.numel() >= max_active,
+          "paged_attend: q and out must be contiguous [max_active, H, hd] of one type")
+    _need(page_table.dim() == 2 and page_table.shape[0] == n_seq,
+          "paged_attend: page_table must be [n_seq, max_pages]")
+    _need(key_len is None or key_len.numel() == n_seq, "paged_attend: one key_len for each sequence")
+    _need(key_live is None or (key_live.dtype == torch.uint8 and key_live.is_contiguous() and
+                               key_live.numel() == kv.n_pages * kv.page_size),
+          "paged_attend: key_live must be uint8, one for each slot")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    scale = 1.0 / math.sqrt(hd) if scale is None else scale
+    _check(lib().adept_paged_attend(dtype_code(q), ctypes.byref(kv), H, scale, int(bool(causal)),
+                                    ptr(q), ptr(rows), ptr(n_active), max_active, ptr(pos),
+                                    ptr(seq), n_seq, ptr(page_table), page_table.shape[1],
+                                    ptr(key_len), ptr(key_live), ptr(out), ptr(workspace), ws_bytes,
+                                    stream_handle(stream)), "adept_paged_attend")
 
 
 def layer_workspace_bytes(args: LayerArgs):

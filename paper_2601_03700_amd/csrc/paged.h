@@ -1,0 +1,61 @@
+// Paged caches: what the store, the load and the attention share.
+#pragma once
+
+#include "common.h"
+
+namespace adept {
+
+// Scale bytes: 127 + E, -100 <= E <= 100.  Inside that range a code times its
+// scale is a normal bf16 and f32 number and so is the scale's inverse.
+constexpr int kScaleMin = 127 - 100, kScaleMax = 127 + 100;
+__device__ __forceinline__ float scale_of(uint8_t byte) { return __uint_as_float((uint32_t)byte << 23); }
+
+// Two e4m3 codes (the low or the high half of w) times a power of two: exact
+// in bf16 and in f32.
+template <bool HI>
+__device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
+}
+template <bool HI>
+__device__ __forceinline__ float2 fp8x2_to_f32x2(uint32_t w, float scale) {
+  const auto f = __builtin_amdgcn_cvt_pk_f32_fp8(w, HI);
+  return make_float2(f[0] * scale, f[1] * scale);
+}
+
+// One layer's pages as a kernel sees them.
+struct PagedView {
+  const void *k, *v;
+  const uint8_t *k_scale, *v_scale;
+  const int32_t* table;   // [n_seq][max_pages]
+  const uint8_t* live;    // by slot, nullable
+  int max_pages, n_pages, shift, n_kv_heads, n_seq;
+  // slot of token t (0 <= t < max_pages << shift) of a sequence; -1: no key there
+  __device__ __forceinline__ int slot(const int32_t* __restrict__ pages, int t) const {
+    const int page = pages[t >> shift];
+    if ((unsigned)page >= (unsigned)n_pages) return -1;
+    const int s = (page << shift) | (t & ((1 << shift) - 1));
+    return live && !live[s] ? -1 : s;
+  }
+};
+
+// Which keys an entry sees: tokens 0 .. limit-1 of its sequence.
+struct Entries {
+  const int32_t *rows, *n_active, *pos, *seq, *key_len;
+  int max_active, causal;
+};
+__device__ __forceinline__ int entry_limit(const Entries& e, const PagedView& c, int row, int* seq) {
+  const int b = e.seq[row];
+  *seq = b;
+  if ((unsigned)b >= (unsigned)c.n_seq) return 0;
+  int n = c.max_pages << c.shift;
+  if (e.causal) n = min(n, min(e.pos[row], INT_MAX - 1) + 1);
+  if (e.key_len) n = min(n, e.key_len[b]);
+  return max(n, 0);
+}
+
+constexpr int kMaxEntries = 1 << 23;   // rows or entries of a call (its grid's bound)
+inline int64_t paged_slots(const adept_paged_kv& kv) { return (int64_t)kv.n_pages * kv.page_size; }
+// the checks of a cache descriptor; `what` names the entry point
+adept_status paged_check(const char* what, adept_dtype dt, const adept_paged_kv* kv);
+
+}  // namespace adept
