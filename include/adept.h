@@ -347,7 +347,7 @@ adept_status adept_attend(adept_dtype dt, int n_heads, int head_dim, float scale
  * the bit.  Reading back is exact in either source type (4 significant bits).
  *
  * page_size is a power of two (1 .. 1024), head_dim a power of two (16 .. 256),
- * n_pages * page_size below 2^31; k, v and the scales 16-byte aligned.  A call
+ * n_pages * page_size below 2^31 - 1023; k, v and the scales 16-byte aligned.  A call
  * takes at most 2^23 rows or entries.
  * ------------------------------------------------------------------------- */
 typedef enum { ADEPT_KV_F32 = 0, ADEPT_KV_BF16 = 1, ADEPT_KV_FP8 = 2 } adept_kv_dtype;
@@ -392,7 +392,7 @@ adept_status adept_paged_load(adept_dtype dt, const adept_paged_kv* kv, const in
  *  key_len is given (nullable); causal=0: to tokens 0 .. key_len[seq]-1.
  *  page_table [n_seq][max_pages] int32: a page outside 0 .. n_pages-1 holds no
  *  keys; nothing behind max_pages * page_size tokens is seen (a product below
- *  2^31).  Entries that no query reaches are not read as pages.
+ *  2^31 - 1023).  Entries that no query reaches are not read as pages.
  *  key_live [n_pages*page_size] uint8, by slot, nullable: slots with 0 are
  *  left out.
  *  out [max_active][H][hd] (dt): softmax(q K^T * scale) V per head, scores and

@@ -29,12 +29,13 @@ struct PagedView {
   const int32_t* table;   // [n_seq][max_pages]
   const uint8_t* live;    // by slot, nullable
   int max_pages, n_pages, shift, n_kv_heads, n_seq;
-  // slot of token t (0 <= t < max_pages << shift) of a sequence; -1: no key there
-  __device__ __forceinline__ int slot(const int32_t* __restrict__ pages, int t) const {
-    const int page = pages[t >> shift];
-    if ((unsigned)page >= (unsigned)n_pages) return -1;
-    const int s = (page << shift) | (t & ((1 << shift) - 1));
-    return live && !live[s] ? -1 : s;
+  // Slot of token t of a sequence from its page's number (-1: no key there).
+  // Loops load the number a block ahead and ask for the slot when it is needed,
+  // so that nothing waits for the load in between.
+  __device__ __forceinline__ int slot(int page, int t, bool in) const {
+    int s = in && (unsigned)page < (unsigned)n_pages ? (page << shift) | (t & ((1 << shift) - 1)) : -1;
+    if (live) s = s >= 0 && live[s] ? s : -1;
+    return s;
   }
 };
 
@@ -54,6 +55,8 @@ __device__ __forceinline__ int entry_limit(const Entries& e, const PagedView& c,
 }
 
 constexpr int kMaxEntries = 1 << 23;   // rows or entries of a call (its grid's bound)
+// slots of a cache and tokens of a sequence: a few blocks past them stay an int
+constexpr int64_t kMaxTokens = INT_MAX - 1023;
 inline int64_t paged_slots(const adept_paged_kv& kv) { return (int64_t)kv.n_pages * kv.page_size; }
 // the checks of a cache descriptor; `what` names the entry point
 adept_status paged_check(const char* what, adept_dtype dt, const adept_paged_kv* kv);

@@ -54,7 +54,7 @@ __device__ __forceinline__ Walk<R> walk_keys(const T* __restrict__ q, int hd, fl
     w.o[i] = 0.0f;
   }
   for (int t = t0; t < t1; ++t) {
-    const int s = c.slot(pages, t);
+    const int s = c.slot(pages[t >> c.shift], t, true);
     if (s < 0) continue;
     const int64_t row = (int64_t)s * c.n_kv_heads + hk;
     float x = 0.0f, v[R];
@@ -241,7 +241,9 @@ __device__ __forceinline__ void column_of(const Tile& t, int j, int G, int hk, i
 // on its way while block kb is computed.  A bf16 cache is copied there by
 // direct loads; an 8-bit one goes through registers, where its codes become
 // bf16 with their scale in the conversion itself (exactly).  The slot of key
-// t0 + lane is found by every wave one block ahead; its ballot is the mask of
+// t0 + lane is found by every wave (its page read a block earlier: the wait for
+// it would be one for all loads on their way, 519 us against 451 for 8 prompts of
+// 2048 tokens); its ballot is the mask of
 // the keys that are there, and the others' rows are read from a row of zeros,
 // so that they add nothing whatever the cache holds.
 //
@@ -342,11 +344,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
       for (int v = 0; v < 16; ++v) o[i][v] = 0.0f;
     float m_ref = -INFINITY, l_run = 0.0f;
 
-    // slots of a block's keys, one per lane
-    auto slots_of = [&](int kb) {
-      const int t = tb + kb * KB + lane;
-      return t < te ? c.slot(pages, t) : -1;
-    };
+    // keys of a block, one per lane; block kb + 1's pages are read during block kb - 1
+    auto key_of = [&](int kb) { return tb + kb * KB + lane; };
+    auto page_of = [&](int kb) { return pages[min(key_of(kb), te - 1) >> c.shift]; };
+    auto slots_of = [&](int kb, int page) { return c.slot(page, key_of(kb), key_of(kb) < te); };
     const int64_t rowc = (int64_t)c.n_kv_heads * HD;    // elements of a slot
     // bf16: direct loads
     auto issue = [&](int u, int sl) {
@@ -408,17 +409,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
     };
 
     uint64_t there = 0;
-    int sl = -1;
+    int page = 0;
     if (nkb > 0) {
-      sl = slots_of(0);
+      const int sl = slots_of(0, page_of(0));
       there = __ballot(sl >= 0);
+      page = page_of(1);
       if constexpr (FP8) {
         fetch(sl);
         put(0);
       } else {
         issue(0, sl);
       }
-      sl = nkb > 1 ? slots_of(1) : -1;
     }
     __syncthreads();
     for (int kb = 0; kb < nkb; ++kb) {
@@ -426,9 +427,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
       const uint64_t mask = there;
       // the other stage was last read in block kb - 1
       if (kb + 1 < nkb) {
+        const int sl = slots_of(kb + 1, page);
         there = __ballot(sl >= 0);
+        page = page_of(kb + 2);
         if constexpr (FP8) fetch(sl); else issue(u ^ 1, sl);
-        sl = kb + 2 < nkb ? slots_of(kb + 2) : -1;
       }
       if (t0 < wend) {
         const char* cK = sKV[u][0];
@@ -636,6 +638,390 @@ bool tiles_fit(adept_dtype dt, const adept_paged_kv& kv) {
   return dt == ADEPT_BF16 && (kv.head_dim == 64 || kv.head_dim == 128);
 }
 
+// ---------------------------------------------------------------------------
+// steps: one entry per sequence
+// ---------------------------------------------------------------------------
+constexpr int SK = 32;             // keys of a wave's block
+constexpr int kStepUnit = 4 * SK;  // keys of a workgroup's block: the unit of the cut
+constexpr int kStepEntries = 1024; // entries up to which long ones are cut
+constexpr int SC = 16;             // columns
+
+__device__ __forceinline__ float max_column(float m) {   // over lanes l, l^16, l^32, l^48
+  const uint32_t u = __float_as_uint(m);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return max_halves(max3_raw(m, __uint_as_float(a[0]), __uint_as_float(a[1])));
+}
+
+// Item x of the call: a stretch of one entry's keys.  Every workgroup finds its
+// own: entries of all workgroups' keys together, cut into about `want` stretches
+// of equal length (whole units; an entry without keys is one), so that a batch of
+// uneven lengths keeps the card evenly loaded.  All threads return the same.
+struct Stretch {
+  int k, part, parts, seq, t0, t1;
+};
+__device__ __forceinline__ Stretch step_stretch(const Entries& e, const PagedView& c, int n, int x,
+                                                int want) {
+  constexpr int P = kStepEntries / 256;
+  __shared__ long long s_sum[4];
+  __shared__ int s_cnt[4], s_out[6];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (n > kStepEntries) {
+    Stretch r{x, 0, 1, 0, 0, 0};
+    if (x >= n) r.parts = 0;
+    else r.t1 = entry_limit(e, c, e.rows[x], &r.seq);
+    return r;
+  }
+  int lim[P], seq[P], units[P];
+  long long sum = 0;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int k = tid * P + i;
+    lim[i] = k < n ? entry_limit(e, c, e.rows[k], &seq[i]) : 0;
+    units[i] = (int)(((long long)lim[i] + kStepUnit - 1) / kStepUnit);
+    sum += units[i];
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if (lane == 0) s_sum[wave] = sum;
+  if (tid < 6) s_out[tid] = 0;
+  __syncthreads();
+  sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+  const int cut = (int)max((sum + want - 1) / want, 1ll);   // units of a stretch
+  int cnt = 0;
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    cnt += tid * P + i < n ? max((units[i] + cut - 1) / cut, 1) : 0;
+  int scan = cnt;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(scan, o, 64);
+    if (lane >= o) scan += y;
+  }
+  if (lane == 63) s_cnt[wave] = scan;
+  __syncthreads();
+  int at = scan - cnt;
+  for (int w = 0; w < wave; ++w) at += s_cnt[w];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int parts = tid * P + i < n ? max((units[i] + cut - 1) / cut, 1) : 0;
+    if (x >= at && x < at + parts) {
+      s_out[0] = tid * P + i;
+      s_out[1] = x - at;
+      s_out[2] = parts;
+      s_out[3] = seq[i];
+      const long long t0 = (long long)(x - at) * cut * kStepUnit;
+      s_out[4] = (int)t0;
+      s_out[5] = (int)min((long long)lim[i], t0 + (long long)cut * kStepUnit);
+    }
+    at += parts;
+  }
+  __syncthreads();
+  return Stretch{s_out[0], s_out[1], s_out[2], s_out[3], s_out[4], s_out[5]};
+}
+
+// One workgroup per (stretch of an entry's keys, K/V head, 16 of its query
+// heads).  The query heads are the columns of 16x16x32 products (one of 16 where
+// heads are not shared: the products cost a small part of the time that the
+// keys take to arrive).  Wave w takes every fourth block of 32 keys from block w
+// on: K straight into registers as the A operand of S^T = K Q^T, V through
+// registers into the wave's own rows of LDS, from which it is read transposed as
+// the A operand of O^T += V^T P^T; no barrier in the loop.  The loads of the next
+// block go out as soon as the products have taken the K registers and LDS the V
+// ones, so a wave has a block in flight (16 KB, 8 KB in 8 bits) while it computes.
+// The four waves' results are joined in LDS; a stretch that is not all of its
+// entry's keys leaves (m, l, o) for paged_step_join_kernel.  The pages of the
+// block after that are read then too, a whole block before their slots are
+// needed (64 sequences of 4096 keys in 8 bits: 477 us, 756 where the slots were
+// formed at once, which waits for every load before).
+template <int HD, bool FP8>
+__global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, int want,
+                                                         float scale_log2,
+                                                         const bf16* __restrict__ q, Entries e,
+                                                         PagedView c, bf16* __restrict__ out,
+                                                         int2* __restrict__ spans,
+                                                         float* __restrict__ part) {
+  constexpr int DS = HD / 32;                      // 32-dim steps of S
+  constexpr int DB = HD / 16;                      // 16-dim blocks of O^T
+  constexpr int ROWB = HD * 2;                     // bytes of a V row in LDS
+  constexpr int ESZ = FP8 ? 1 : 2;
+  constexpr int NCH = HD * ESZ / 16;               // 16-byte pieces of a cache row
+  constexpr int KP = NCH / 4;                      // K pieces of a lane and 16 keys
+  constexpr int RPI = 64 / NCH;                    // V rows of one load of a wave
+  constexpr int VI = SK / RPI;                     // loads of V
+  __shared__ __attribute__((aligned(16))) char sV[4][SK * ROWB];
+  __shared__ float s_m[4][SC], s_l[4][SC];
+  // heads of one stretch side by side
+  const int hk = blockIdx.x % c.n_kv_heads, cg = blockIdx.x / c.n_kv_heads % col_groups;
+  const int x = blockIdx.x / (c.n_kv_heads * col_groups);
+  const int n = min(*e.n_active, e.max_active);
+  const Stretch st = step_stretch(e, c, n, x, want);
+  if (st.parts == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, c16 = lane & 15;
+  const int G = H / c.n_kv_heads, cols = min(SC, G - cg * SC);
+  const int h0 = hk * G + cg * SC;                 // query head of column 0
+  const int64_t qat = ((int64_t)st.k * H + h0) * HD;
+  const int32_t* pages = c.table + (int64_t)st.seq * c.max_pages;
+  const int64_t rowc = (int64_t)c.n_kv_heads * HD;
+  const char* kbase = (const char*)c.k + hk * HD * ESZ;
+  const char* vbase = (const char*)c.v + hk * HD * ESZ;
+
+  // Q as the B operand, its dims in the order in which a lane's K pieces come:
+  // a piece of a bf16 row holds 8 dims of one step, of an 8-bit row 16 dims of two
+  bf16x8_t qf[DS];
+#pragma unroll
+  for (int s = 0; s < DS; ++s) {
+    const int d = FP8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+    qf[s] = __builtin_bit_cast(
+        bf16x8_t, c16 < cols ? *reinterpret_cast<const uint4*>(q + qat + c16 * HD + d)
+                             : make_uint4(0, 0, 0, 0));
+  }
+  f32x4_t o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m_ref = -INFINITY, l_run = 0.0f;
+
+  const int nblk = (st.t1 - st.t0 + kStepUnit - 1) / kStepUnit;   // blocks of each wave
+  // keys of block i, one per lane (the upper half of the wave again), the pages
+  // of block i + 1 read while block i's rows are on their way
+  auto key_of = [&](int i) { return st.t0 + (i * 4 + wave) * SK + (lane & 31); };
+  auto page_of = [&](int i) { return pages[min(key_of(i), st.t1 - 1) >> c.shift]; };
+  auto slots_of = [&](int i, int page) { return c.slot(page, key_of(i), key_of(i) < st.t1); };
+  uint4 kr[2][KP], vr[VI];
+  uint8_t ksc[2], vsc[VI];     // scale bytes
+  // a key that is not there: slot 0 is read in its place, its score masked and
+  // its V row cleared (drop_rows)
+  auto fetch = [&](int sl) {
+    const int sc = max(sl, 0);
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb) {
+      const int s = __shfl(sc, sb * 16 + c16, 64);
+      const char* src = kbase + s * rowc * ESZ + g * 16;
+#pragma unroll
+      for (int i = 0; i < KP; ++i) kr[sb][i] = *reinterpret_cast<const uint4*>(src + i * 64);
+      if constexpr (FP8) ksc[sb] = c.k_scale[(int64_t)s * c.n_kv_heads + hk];
+    }
+#pragma unroll
+    for (int i = 0; i < VI; ++i) {
+      const int s = __shfl(sc, i * RPI + lane / NCH, 64);
+      vr[i] = *reinterpret_cast<const uint4*>(vbase + s * rowc * ESZ + lane % NCH * 16);
+      if constexpr (FP8) vsc[i] = c.v_scale[(int64_t)s * c.n_kv_heads + hk];
+    }
+  };
+  auto drop_rows = [&](uint32_t there) {
+#pragma unroll
+    for (int i = 0; i < VI; ++i)
+      if (!((there >> (i * RPI + lane / NCH)) & 1)) vr[i] = make_uint4(0, 0, 0, 0);
+  };
+  auto fv = [](int r) { return HD == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); };
+  auto wide = [](uint32_t a, uint32_t b, uint8_t byte) {    // 8 codes to 8 bf16
+    const float sc = scale_of(byte);
+    return make_uint4(fp8x2_to_bf16x2<false>(a, sc), fp8x2_to_bf16x2<true>(a, sc),
+                      fp8x2_to_bf16x2<false>(b, sc), fp8x2_to_bf16x2<true>(b, sc));
+  };
+
+  int page = 0;
+  uint32_t there = 0;
+  if (nblk > 0) {
+    const int sl = slots_of(0, page_of(0));
+    there = (uint32_t)__ballot(sl >= 0);
+    page = page_of(1);
+    fetch(sl);
+  }
+  for (int i = 0; i < nblk; ++i) {
+    const uint32_t mask = there;
+    f32x4_t s[2];
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb) {
+      s[sb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) {
+        uint4 a;
+        if constexpr (FP8) {
+          const uint4 w = kr[sb][ds >> 1];
+          a = ds & 1 ? wide(w.z, w.w, ksc[sb]) : wide(w.x, w.y, ksc[sb]);
+        } else {
+          a = kr[sb][ds];
+        }
+        s[sb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), qf[ds],
+                                                        s[sb], 0, 0, 0);
+      }
+    }
+    if (mask != ~0u) drop_rows(mask);
+#pragma unroll
+    for (int j = 0; j < VI; ++j) {
+      const int r = j * RPI + lane / NCH, ch = lane % NCH;
+      char* row = sV[wave] + r * ROWB;
+      if constexpr (FP8) {
+        *reinterpret_cast<uint4*>(row + ((2 * ch) ^ fv(r)) * 16) = wide(vr[j].x, vr[j].y, vsc[j]);
+        *reinterpret_cast<uint4*>(row + ((2 * ch + 1) ^ fv(r)) * 16) = wide(vr[j].z, vr[j].w, vsc[j]);
+      } else {
+        *reinterpret_cast<uint4*>(row + (ch ^ fv(r)) * 16) = vr[j];
+      }
+    }
+    if (i + 1 < nblk) {
+      const int sl = slots_of(i + 1, page);
+      there = (uint32_t)__ballot(sl >= 0);
+      page = page_of(i + 2);
+      fetch(sl);
+    }
+    if (mask != ~0u) {       // keys that are not there, or behind the stretch
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          s[sb][v] = (mask >> (sb * 16 + 4 * g + v)) & 1 ? s[sb][v] : -INFINITY;
+    }
+    float mb = max3_raw(s[0][0], s[0][1], s[0][2]);
+    mb = max3_raw(mb, s[0][3], s[1][0]);
+    mb = max3_raw(mb, s[1][1], s[1][2]);
+    mb = max_column(max3_raw(mb, s[1][3], mb)) * scale_log2;
+    if (__any(mb > m_ref + kLazy)) {
+      const float mn = fmaxf(m_ref, mb);
+      const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_ref - mn);
+      m_ref = mn;
+      l_run *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[d][v] *= alpha;
+    }
+    const float msub = m_ref == -INFINITY ? 0.0f : m_ref;
+    constexpr bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
+    uint32_t w[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const float a = s[y >> 1][2 * (y & 1)], b = s[y >> 1][2 * (y & 1) + 1];
+      w[y] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(a, scale_log2, -msub)),
+                         __builtin_amdgcn_exp2f(fmaf(b, scale_log2, -msub)));
+      l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[y]), ones, l_run, false);
+    }
+    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      s16x4 half[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int r = 16 * y + 4 * g + (c16 >> 2);
+        const int ch = 2 * db + ((c16 & 3) >> 1);
+        half[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4*)(sV[wave] + r * ROWB + ((ch ^ fv(r)) * 16) + 8 * (c16 & 1)));
+      }
+      const bf16x8_t a = __builtin_bit_cast(
+          bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+      o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb, o[db], 0, 0, 0);
+    }
+  }
+
+  // the four waves' results
+  float l = l_run;
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  float* so = (float*)sV[wave];       // [SC][HD]: a wave's V rows hold SK * HD bf16
+  static_assert(SC * HD * 4 <= SK * ROWB, "a wave's output fits its V rows");
+  if (c16 < cols) {
+    if (g == 0) {
+      s_m[wave][c16] = m_ref;
+      s_l[wave][c16] = l;
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+      *reinterpret_cast<f32x4_t*>(so + c16 * HD + db * 16 + g * 4) = o[db];
+  }
+  __syncthreads();
+  const bool whole = st.parts == 1;
+  const int64_t at = ((int64_t)x * c.n_kv_heads + hk) * G + cg * SC;   // of the partial results
+  for (int j = tid / (HD / 4); j < cols; j += 256 / (HD / 4)) {
+    const int d = tid % (HD / 4) * 4;
+    float m = s_m[0][j];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][j]);
+    float ls = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      // a wave without keys has l = 0 and o = 0: its factor does not matter
+      const float f = s_m[w][j] == m ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][j] - m);
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>((const float*)sV[w] + j * HD + d);
+      ls = fmaf(f, s_l[w][j], ls);
+#pragma unroll
+      for (int z = 0; z < 4; ++z) y[z] = fmaf(f, v[z], y[z]);
+    }
+    if (whole) {
+      const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+      *reinterpret_cast<uint2*>(out + qat + j * HD + d) =
+          make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
+    } else {
+      float* pp = part + (at + j) * (HD + 4);
+      *reinterpret_cast<float4*>(pp + 4 + d) = make_float4(y[0], y[1], y[2], y[3]);
+      if (d == 0) *reinterpret_cast<float2*>(pp) = make_float2(m, ls);
+    }
+  }
+  if (tid == 0 && st.part == 0 && hk == 0 && cg == 0) spans[st.k] = make_int2(x, st.parts);
+}
+
+// Joins the stretches of each entry that has several.
+template <int HD>
+__global__ __launch_bounds__(256) void paged_step_join_kernel(int H, Entries e,
+                                                              const int2* __restrict__ spans,
+                                                              const float* __restrict__ part,
+                                                              bf16* __restrict__ out) {
+  constexpr int CPB = 256 / (HD / 4);
+  const int k = blockIdx.x, n = min(*e.n_active, e.max_active);
+  const int h = blockIdx.y * CPB + threadIdx.x / (HD / 4), d = threadIdx.x % (HD / 4) * 4;
+  if (k >= n || h >= H) return;
+  const int2 sp = spans[k];
+  if (sp.y <= 1) return;
+  const float* pp = part + ((int64_t)sp.x * H + h) * (HD + 4);
+  const int64_t step = (int64_t)H * (HD + 4);
+  float m = -INFINITY;
+#pragma unroll 4
+  for (int p = 0; p < sp.y; ++p) m = fmaxf(m, pp[p * step]);
+  float l = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < sp.y; ++p) {
+    const float2 ml = *reinterpret_cast<const float2*>(pp + p * step);
+    const float4 v = *reinterpret_cast<const float4*>(pp + p * step + 4 + d);
+    const float f = ml.x == m ? 1.0f : __builtin_amdgcn_exp2f(ml.x - m);
+    l = fmaf(f, ml.y, l);
+    y[0] = fmaf(f, v.x, y[0]);
+    y[1] = fmaf(f, v.y, y[1]);
+    y[2] = fmaf(f, v.z, y[2]);
+    y[3] = fmaf(f, v.w, y[3]);
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  *reinterpret_cast<uint2*>(out + ((int64_t)k * H + h) * HD + d) =
+      make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
+}
+
+// want: stretches of the call's keys for each (K/V head, column group)
+struct StepShape {
+  int groups, want, items;
+  bool cut;          // whether an entry can have several stretches
+  size_t off_part, bytes;
+};
+StepShape step_shape(const adept_paged_kv& kv, int n_heads, int max_active, int max_pages) {
+  StepShape t{};
+  const int G = n_heads / kv.n_kv_heads;
+  t.groups = ceil_div(G, SC);
+  const int64_t keys = (int64_t)max_pages * kv.page_size;
+  t.want = std::max(1, 8192 / (kv.n_kv_heads * t.groups));
+  t.cut = keys > kStepUnit;
+  const int64_t most = std::max<int64_t>(1, (keys + kStepUnit - 1) / kStepUnit);
+  t.items = (int)std::min<int64_t>((int64_t)max_active + t.want, max_active * most);
+  t.off_part = ((size_t)max_active * sizeof(int2) + 255) & ~(size_t)255;
+  t.bytes = t.off_part;
+  if (t.cut)
+    t.bytes += ((size_t)std::min(max_active, kStepEntries) + t.want) * n_heads *
+               (kv.head_dim + 4) * sizeof(float);
+  t.bytes = std::max<size_t>(t.bytes, 256);
+  return t;
+}
+// one entry per sequence at most, on average: each reads its keys for itself
+bool step_fits(adept_dtype dt, const adept_paged_kv& kv, int max_active, int n_seq) {
+  return tiles_fit(dt, kv) && max_active <= n_seq;
+}
+
 }  // namespace
 }  // namespace adept
 
@@ -646,7 +1032,8 @@ extern "C" size_t adept_paged_attend_workspace_bytes(const adept_paged_kv* kv, i
   if (!kv || kv->n_kv_heads <= 0 || n_heads < kv->n_kv_heads || max_active < 0 || n_seq <= 0 ||
       max_pages <= 0)
     return 256;
-  return tile_shape(*kv, n_heads, max_active, n_seq, max_pages).bytes;
+  return std::max(tile_shape(*kv, n_heads, max_active, n_seq, max_pages).bytes,
+                  step_shape(*kv, n_heads, max_active, max_pages).bytes);
 }
 
 extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv* kv, int n_heads,
@@ -662,7 +1049,7 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
   ADEPT_REQUIRE(n_heads > 0 && n_heads <= 4096 && n_heads % kv->n_kv_heads == 0,
                 "paged_attend: %d heads are no multiple of %d", n_heads, kv->n_kv_heads);
   ADEPT_REQUIRE(max_active >= 0 && max_active <= kMaxEntries && n_seq > 0 && max_pages > 0 &&
-                    (int64_t)max_pages * kv->page_size <= INT_MAX,
+                    (int64_t)max_pages * kv->page_size <= kMaxTokens,
                 "paged_attend: bad sizes");
   if (max_active == 0) return ADEPT_OK;
   ADEPT_REQUIRE(q && rows && n_active && pos && seq && page_table && out,
@@ -684,6 +1071,33 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
   const float sl = scale * 1.4426950408889634f;   // scores in the exp2 domain
   hipStream_t s = as_stream(stream);
   const bool fp8 = kv->dtype == ADEPT_KV_FP8;
+  if (step_fits(dt, *kv, max_active, n_seq)) {
+    const StepShape ss = step_shape(*kv, n_heads, max_active, max_pages);
+    int2* spans = (int2*)workspace;
+    float* part = (float*)((char*)workspace + ss.off_part);
+    const int64_t items = (int64_t)ss.items * kv->n_kv_heads * ss.groups;
+    ADEPT_REQUIRE(items <= 1 << 23, "paged_attend: too many entries");
+#define ADEPT_STEP(HD, FP8)                                                                       \
+  ADEPT_LAUNCH((paged_step_kernel<HD, FP8>), dim3((unsigned)items), dim3(256), 0, s, n_heads,     \
+               ss.groups, ss.want, sl, (const bf16*)q, e, c, (bf16*)out, spans, part)
+    if (hd == 128) {
+      if (fp8) ADEPT_STEP(128, true); else ADEPT_STEP(128, false);
+    } else {
+      if (fp8) ADEPT_STEP(64, true); else ADEPT_STEP(64, false);
+    }
+#undef ADEPT_STEP
+    ADEPT_CHECK_LAUNCH("paged_step");
+    if (ss.cut) {
+      const dim3 jg(max_active, ceil_div(n_heads, 1024 / hd));
+      if (hd == 128)
+        ADEPT_LAUNCH(paged_step_join_kernel<128>, jg, dim3(256), 0, s, n_heads, e, spans, part,
+                     (bf16*)out);
+      else
+        ADEPT_LAUNCH(paged_step_join_kernel<64>, jg, dim3(256), 0, s, n_heads, e, spans, part,
+                     (bf16*)out);
+    }
+    return launch_status("paged_attend");
+  }
   if (tiles_fit(dt, *kv)) {
     const TileShape ts = tile_shape(*kv, n_heads, max_active, n_seq, max_pages);
     char* w = (char*)workspace;

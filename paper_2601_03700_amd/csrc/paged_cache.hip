@@ -22,7 +22,7 @@ adept_status paged_check(const char* what, adept_dtype dt, const adept_paged_kv*
                 "%s: head_dim %d must be a power of two from 16 to 256", what, hd);
   ADEPT_REQUIRE(ps >= 1 && ps <= 1024 && (ps & (ps - 1)) == 0,
                 "%s: page_size %d must be a power of two from 1 to 1024", what, ps);
-  ADEPT_REQUIRE(kv->n_pages > 0 && paged_slots(*kv) <= INT_MAX, "%s: bad n_pages %d", what,
+  ADEPT_REQUIRE(kv->n_pages > 0 && paged_slots(*kv) <= kMaxTokens, "%s: bad n_pages %d", what,
                 kv->n_pages);
   ADEPT_REQUIRE(kv->k && kv->v && aligned16(kv->k) && aligned16(kv->v),
                 "%s: K and V must be 16-byte aligned", what);
