@@ -362,23 +362,28 @@ _KV_TYPES = {torch.float32: KV_F32, torch.bfloat16: KV_BF16, torch.uint8: KV_FP8
              torch.float8_e4m3fn: KV_FP8}
 
 
-def _need(cond, what):
+def _need(cond, what, why):
     if not cond:
-        raise AdeptError(what)
+        raise AdeptError(f"{what}: {why}")
 
 
 def _need_here(what, *tensors):
     """Tensors on the current device (the library launches on its streams)."""
-    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    here = None
     for t in tensors:
-        _need(t is None or (t.is_cuda and t.device.index == here),
-              f"{what}: tensors must be on the current HIP device")
+        if t is not None:
+            at = t.get_device()
+            if at < 0 or (here is not None and at != here):
+                raise AdeptError(f"{what}: tensors must be on the current HIP device")
+            here = at
+    if here != torch.cuda.current_device():
+        raise AdeptError(f"{what}: tensors must be on the current HIP device")
 
 
 def _need_i32(what, *tensors):
     for t in tensors:
-        _need(t is None or (t.dtype == torch.int32 and t.is_contiguous()),
-              f"{what}: index tensors must be contiguous int32")
+        if t is not None and not (t.dtype is torch.int32 and t.is_contiguous()):
+            raise AdeptError(f"{what}: index tensors must be contiguous int32")
 
 
 def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
@@ -387,15 +392,15 @@ def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
     multiple of page_size.  It holds the tensors."""
     _need(k.dim() == 3 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in _KV_TYPES and
           k.is_contiguous() and v.is_contiguous(),
-          "paged_kv: k and v must be contiguous [n_slots, Hkv, hd] of one cache type")
+          "paged_kv", "k and v must be contiguous [n_slots, Hkv, hd] of one cache type")
     _need(page_size >= 1 and k.shape[0] % page_size == 0,
-          f"paged_kv: {k.shape[0]} slots are no multiple of the page size {page_size}")
+          "paged_kv", f"{k.shape[0]} slots are no multiple of the page size {page_size}")
     fp8 = _KV_TYPES[k.dtype] == KV_FP8
     _need(fp8 == (k_scale is not None) == (v_scale is not None),
-          "paged_kv: scales go with an 8-bit cache, and only with it")
+          "paged_kv", "scales go with an 8-bit cache, and only with it")
     for s in (k_scale, v_scale) if fp8 else ():
         _need(s.dtype == torch.uint8 and s.shape == k.shape[:2] and s.is_contiguous(),
-              "paged_kv: scales must be contiguous uint8 [n_slots, Hkv]")
+              "paged_kv", "scales must be contiguous uint8 [n_slots, Hkv]")
     kv = PagedKv(_KV_TYPES[k.dtype], k.shape[1], k.shape[2], page_size, k.shape[0] // page_size,
                  ptr(k), ptr(v), ptr(k_scale), ptr(v_scale))
     kv.tensors = (k, v, k_scale, v_scale)
@@ -403,13 +408,13 @@ def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
 
 
 def _paged_rows(what, kv, k, v):
-    _need_here(what, *kv.tensors)
-    dims = (kv.n_kv_heads, kv.head_dim)
+    heads, hd = kv.n_kv_heads, kv.head_dim
     for t in (k, v):
-        _need(t.dim() == 3 and tuple(t.shape[1:]) == dims and t.dtype == k.dtype and
-              t.dtype in (torch.float32, torch.bfloat16) and
-              (t.shape[0] == 0 or (t.stride(2) == 1 and t.stride(1) == dims[1])),
-              f"{what}: rows must be f32 or bf16 [n, {dims[0]}, {dims[1]}] with contiguous heads")
+        if not (t.dim() == 3 and t.shape[1] == heads and t.shape[2] == hd and t.dtype is k.dtype and
+                t.dtype in (torch.float32, torch.bfloat16) and
+                (t.shape[0] == 0 or (t.stride(2) == 1 and t.stride(1) == hd))):
+            raise AdeptError(f"{what}: rows must be f32 or bf16 [n, {heads}, {hd}] with contiguous "
+                             "heads")
 
 
 def _row_stride(t):
@@ -422,9 +427,9 @@ def paged_store(kv, k, v, slot, rows=None, n_rows=None, stream=None):
     if it is an 8-bit one; rows: the listed rows only, n_rows (device int32 [1]): how many of
     them."""
     _paged_rows("paged_store", kv, k, v)
-    _need_here("paged_store", k, v, slot, rows, n_rows)
+    _need_here("paged_store", *kv.tensors, k, v, slot, rows, n_rows)
     _need_i32("paged_store", slot, rows, n_rows)
-    _need(k.shape[0] == v.shape[0] == slot.numel(), "paged_store: one slot for each row")
+    _need(k.shape[0] == v.shape[0] == slot.numel(), "paged_store", "one slot for each row")
     n = k.shape[0] if rows is None else rows.numel()
     _check(lib().adept_paged_store(dtype_code(k), ctypes.byref(kv), ptr(k), _row_stride(k), ptr(v),
                                    _row_stride(v), ptr(rows), ptr(n_rows), n, ptr(slot),
@@ -434,10 +439,10 @@ def paged_store(kv, k, v, slot, rows=None, n_rows=None, stream=None):
 def paged_load(kv, slot, k, v, n_rows=None, stream=None):
     """k[i], v[i] = the cache's values at slot[i] (k, v [n, Hkv, hd], any row stride)."""
     _paged_rows("paged_load", kv, k, v)
-    _need_here("paged_load", k, v, slot, n_rows)
+    _need_here("paged_load", *kv.tensors, k, v, slot, n_rows)
     _need_i32("paged_load", slot, n_rows)
     n = slot.numel()
-    _need(k.shape[0] >= n and v.shape[0] >= n, "paged_load: fewer output rows than slots")
+    _need(k.shape[0] >= n and v.shape[0] >= n, "paged_load", "fewer output rows than slots")
     _check(lib().adept_paged_load(dtype_code(k), ctypes.byref(kv), ptr(slot), ptr(n_rows), n, ptr(k),
                                   _row_stride(k), ptr(v), _row_stride(v), stream_handle(stream)),
            "adept_paged_load")
@@ -460,13 +465,13 @@ def paged_attend(kv, q, rows, n_active, max_active, pos, seq, n_seq, page_table,
           q.dtype in (torch.float32, torch.bfloat16) and hd == kv.head_dim and
           q.shape[0] >= max_active and out.numel() >= max_active * H * hd and
           rows.numel() >= max_active,
-          "paged_attend: q and out must be contiguous [max_active, H, hd] of one type")
+          "paged_attend", "q and out must be contiguous [max_active, H, hd] of one type")
     _need(page_table.dim() == 2 and page_table.shape[0] == n_seq,
-          "paged_attend: page_table must be [n_seq, max_pages]")
-    _need(key_len is None or key_len.numel() == n_seq, "paged_attend: one key_len for each sequence")
+          "paged_attend", "page_table must be [n_seq, max_pages]")
+    _need(key_len is None or key_len.numel() == n_seq, "paged_attend", "one key_len for each sequence")
     _need(key_live is None or (key_live.dtype == torch.uint8 and key_live.is_contiguous() and
                                key_live.numel() == kv.n_pages * kv.page_size),
-          "paged_attend: key_live must be uint8, one for each slot")
+          "paged_attend", "key_live must be uint8, one for each slot")
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     scale = 1.0 / math.sqrt(hd) if scale is None else scale
     _check(lib().adept_paged_attend(dtype_code(q), ctypes.byref(kv), H, scale, int(bool(causal)),

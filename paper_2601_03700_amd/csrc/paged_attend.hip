@@ -197,6 +197,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Entries e, int
 // tiles
 // ---------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 constexpr float kLazy = 8.0f;   // log2 headroom of the reference maximum
@@ -645,6 +646,10 @@ constexpr int SK = 32;             // keys of a wave's block
 constexpr int kStepUnit = 4 * SK;  // keys of a workgroup's block: the unit of the cut
 constexpr int kStepEntries = 1024; // entries up to which long ones are cut
 constexpr int SC = 16;             // columns
+// Workgroups that a call is cut into, about: 40 uneven sequences (8 K/V heads)
+// 119 us with 2048, 131 with 4096, 153 with 8192 (a workgroup starts with some
+// five dependent loads); 64 sequences of 4096 keys, 32 heads, 653, 641 and 663 us.
+constexpr int kStepItems = 2048;
 
 __device__ __forceinline__ float max_column(float m) {   // over lanes l, l^16, l^32, l^48
   const uint32_t u = __float_as_uint(m);
@@ -723,18 +728,20 @@ __device__ __forceinline__ Stretch step_stretch(const Entries& e, const PagedVie
 // heads).  The query heads are the columns of 16x16x32 products (one of 16 where
 // heads are not shared: the products cost a small part of the time that the
 // keys take to arrive).  Wave w takes every fourth block of 32 keys from block w
-// on: K straight into registers as the A operand of S^T = K Q^T, V through
-// registers into the wave's own rows of LDS, from which it is read transposed as
-// the A operand of O^T += V^T P^T; no barrier in the loop.  The loads of the next
-// block go out as soon as the products have taken the K registers and LDS the V
-// ones, so a wave has a block in flight (16 KB, 8 KB in 8 bits) while it computes.
+// on, whole rows at a time (16 bytes a lane), through registers into the wave's own
+// 32 rows of LDS: K, read back as the A operand of S^T = K Q^T, then V over it,
+// read transposed as the A operand of O^T += V^T P^T; no barrier in the loop.
+// The loads of the next block go out as soon as LDS has taken this one's, so a
+// wave has a block in flight (16 KB, 8 KB in 8 bits) while it computes.  (K
+// loaded as operands, 64 bytes of 16 rows at a
+// time, halves of lines: 64 sequences of 4096 keys 770 us, 653 so.)
 // The four waves' results are joined in LDS; a stretch that is not all of its
 // entry's keys leaves (m, l, o) for paged_step_join_kernel.  The pages of the
 // block after that are read then too, a whole block before their slots are
 // needed (64 sequences of 4096 keys in 8 bits: 477 us, 756 where the slots were
 // formed at once, which waits for every load before).
 template <int HD, bool FP8>
-__global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, int want,
+__global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kernel(int H, int col_groups, int want,
                                                          float scale_log2,
                                                          const bf16* __restrict__ q, Entries e,
                                                          PagedView c, bf16* __restrict__ out,
@@ -745,14 +752,13 @@ __global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, 
   constexpr int ROWB = HD * 2;                     // bytes of a V row in LDS
   constexpr int ESZ = FP8 ? 1 : 2;
   constexpr int NCH = HD * ESZ / 16;               // 16-byte pieces of a cache row
-  constexpr int KP = NCH / 4;                      // K pieces of a lane and 16 keys
-  constexpr int RPI = 64 / NCH;                    // V rows of one load of a wave
-  constexpr int VI = SK / RPI;                     // loads of V
-  __shared__ __attribute__((aligned(16))) char sV[4][SK * ROWB];
+  constexpr int RPI = 64 / NCH;                    // rows of one load of a wave
+  constexpr int RI = SK / RPI;                     // loads of K, and of V
+  __shared__ __attribute__((aligned(16))) char s_rows[4][SK * ROWB];
   __shared__ float s_m[4][SC], s_l[4][SC];
-  // heads of one stretch side by side
-  const int hk = blockIdx.x % c.n_kv_heads, cg = blockIdx.x / c.n_kv_heads % col_groups;
-  const int x = blockIdx.x / (c.n_kv_heads * col_groups);
+  const int items = gridDim.x / (c.n_kv_heads * col_groups);   // stretches side by side
+  const int x = blockIdx.x % items, hk = blockIdx.x / items % c.n_kv_heads,
+            cg = blockIdx.x / items / c.n_kv_heads;
   const int n = min(*e.n_active, e.max_active);
   const Stretch st = step_stretch(e, c, n, x, want);
   if (st.parts == 0) return;
@@ -764,19 +770,16 @@ __global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, 
   const int64_t qat = ((int64_t)st.k * H + h0) * HD;
   const int32_t* pages = c.table + (int64_t)st.seq * c.max_pages;
   const int64_t rowc = (int64_t)c.n_kv_heads * HD;
+  char* rows = s_rows[wave];
   const char* kbase = (const char*)c.k + hk * HD * ESZ;
   const char* vbase = (const char*)c.v + hk * HD * ESZ;
 
-  // Q as the B operand, its dims in the order in which a lane's K pieces come:
-  // a piece of a bf16 row holds 8 dims of one step, of an 8-bit row 16 dims of two
-  bf16x8_t qf[DS];
+  bf16x8_t qf[DS];     // the B operand
 #pragma unroll
-  for (int s = 0; s < DS; ++s) {
-    const int d = FP8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+  for (int s = 0; s < DS; ++s)
     qf[s] = __builtin_bit_cast(
-        bf16x8_t, c16 < cols ? *reinterpret_cast<const uint4*>(q + qat + c16 * HD + d)
+        bf16x8_t, c16 < cols ? *reinterpret_cast<const uint4*>(q + qat + c16 * HD + s * 32 + g * 8)
                              : make_uint4(0, 0, 0, 0));
-  }
   f32x4_t o[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -788,37 +791,31 @@ __global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, 
   auto key_of = [&](int i) { return st.t0 + (i * 4 + wave) * SK + (lane & 31); };
   auto page_of = [&](int i) { return pages[min(key_of(i), st.t1 - 1) >> c.shift]; };
   auto slots_of = [&](int i, int page) { return c.slot(page, key_of(i), key_of(i) < st.t1); };
-  uint4 kr[2][KP], vr[VI];
-  uint8_t ksc[2], vsc[VI];     // scale bytes
+  u32x4_t kr[RI], vr[RI];
+  uint8_t ksc[RI], vsc[RI];     // scale bytes
   // a key that is not there: slot 0 is read in its place, its score masked and
-  // its V row cleared (drop_rows)
+  // its V row cleared
   auto fetch = [&](int sl) {
     const int sc = max(sl, 0);
 #pragma unroll
-    for (int sb = 0; sb < 2; ++sb) {
-      const int s = __shfl(sc, sb * 16 + c16, 64);
-      const char* src = kbase + s * rowc * ESZ + g * 16;
-#pragma unroll
-      for (int i = 0; i < KP; ++i) kr[sb][i] = *reinterpret_cast<const uint4*>(src + i * 64);
-      if constexpr (FP8) ksc[sb] = c.k_scale[(int64_t)s * c.n_kv_heads + hk];
-    }
-#pragma unroll
-    for (int i = 0; i < VI; ++i) {
+    for (int i = 0; i < RI; ++i) {
       const int s = __shfl(sc, i * RPI + lane / NCH, 64);
-      vr[i] = *reinterpret_cast<const uint4*>(vbase + s * rowc * ESZ + lane % NCH * 16);
-      if constexpr (FP8) vsc[i] = c.v_scale[(int64_t)s * c.n_kv_heads + hk];
+      const int64_t at = s * rowc * ESZ + lane % NCH * 16;
+      // read once (by this entry)
+      kr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kbase + at));
+      vr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vbase + at));
+      if constexpr (FP8) {
+        ksc[i] = c.k_scale[(int64_t)s * c.n_kv_heads + hk];
+        vsc[i] = c.v_scale[(int64_t)s * c.n_kv_heads + hk];
+      }
     }
   };
-  auto drop_rows = [&](uint32_t there) {
-#pragma unroll
-    for (int i = 0; i < VI; ++i)
-      if (!((there >> (i * RPI + lane / NCH)) & 1)) vr[i] = make_uint4(0, 0, 0, 0);
-  };
+  auto fk = [](int r) { return HD == 128 ? (r & 15) : ((r >> 1) & 7); };
   auto fv = [](int r) { return HD == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); };
   auto wide = [](uint32_t a, uint32_t b, uint8_t byte) {    // 8 codes to 8 bf16
     const float sc = scale_of(byte);
-    return make_uint4(fp8x2_to_bf16x2<false>(a, sc), fp8x2_to_bf16x2<true>(a, sc),
-                      fp8x2_to_bf16x2<false>(b, sc), fp8x2_to_bf16x2<true>(b, sc));
+    return u32x4_t{fp8x2_to_bf16x2<false>(a, sc), fp8x2_to_bf16x2<true>(a, sc),
+                   fp8x2_to_bf16x2<false>(b, sc), fp8x2_to_bf16x2<true>(b, sc)};
   };
 
   int page = 0;
@@ -831,35 +828,38 @@ __global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, 
   }
   for (int i = 0; i < nblk; ++i) {
     const uint32_t mask = there;
+    // rows into LDS, chunk c of row r at c ^ f(r)
+    auto put = [&](const u32x4_t (&x)[RI], const uint8_t (&sc)[RI], auto f) {
+#pragma unroll
+      for (int j = 0; j < RI; ++j) {
+        const int r = j * RPI + lane / NCH, ch = lane % NCH;
+        char* row = rows + r * ROWB;
+        if constexpr (FP8) {
+          *reinterpret_cast<u32x4_t*>(row + ((2 * ch) ^ f(r)) * 16) = wide(x[j][0], x[j][1], sc[j]);
+          *reinterpret_cast<u32x4_t*>(row + ((2 * ch + 1) ^ f(r)) * 16) = wide(x[j][2], x[j][3], sc[j]);
+        } else {
+          *reinterpret_cast<u32x4_t*>(row + (ch ^ f(r)) * 16) = x[j];
+        }
+      }
+    };
+    put(kr, ksc, fk);
     f32x4_t s[2];
 #pragma unroll
     for (int sb = 0; sb < 2; ++sb) {
       s[sb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const int r = sb * 16 + c16;
 #pragma unroll
       for (int ds = 0; ds < DS; ++ds) {
-        uint4 a;
-        if constexpr (FP8) {
-          const uint4 w = kr[sb][ds >> 1];
-          a = ds & 1 ? wide(w.z, w.w, ksc[sb]) : wide(w.x, w.y, ksc[sb]);
-        } else {
-          a = kr[sb][ds];
-        }
-        s[sb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), qf[ds],
-                                                        s[sb], 0, 0, 0);
+        const bf16x8_t a =
+            *reinterpret_cast<const bf16x8_t*>(rows + r * ROWB + ((4 * ds + g) ^ fk(r)) * 16);
+        s[sb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[ds], s[sb], 0, 0, 0);
       }
     }
-    if (mask != ~0u) drop_rows(mask);
+    if (mask != ~0u)
 #pragma unroll
-    for (int j = 0; j < VI; ++j) {
-      const int r = j * RPI + lane / NCH, ch = lane % NCH;
-      char* row = sV[wave] + r * ROWB;
-      if constexpr (FP8) {
-        *reinterpret_cast<uint4*>(row + ((2 * ch) ^ fv(r)) * 16) = wide(vr[j].x, vr[j].y, vsc[j]);
-        *reinterpret_cast<uint4*>(row + ((2 * ch + 1) ^ fv(r)) * 16) = wide(vr[j].z, vr[j].w, vsc[j]);
-      } else {
-        *reinterpret_cast<uint4*>(row + (ch ^ fv(r)) * 16) = vr[j];
-      }
-    }
+      for (int j = 0; j < RI; ++j)
+        if (!((mask >> (j * RPI + lane / NCH)) & 1)) vr[j] = u32x4_t{0, 0, 0, 0};
+    put(vr, vsc, fv);      // over K: a wave's LDS accesses keep their order
     if (i + 1 < nblk) {
       const int sl = slots_of(i + 1, page);
       there = (uint32_t)__ballot(sl >= 0);
@@ -906,7 +906,7 @@ __global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, 
         const int r = 16 * y + 4 * g + (c16 >> 2);
         const int ch = 2 * db + ((c16 & 3) >> 1);
         half[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4*)(sV[wave] + r * ROWB + ((ch ^ fv(r)) * 16) + 8 * (c16 & 1)));
+            (lds_s16x4*)(rows + r * ROWB + ((ch ^ fv(r)) * 16) + 8 * (c16 & 1)));
       }
       const bf16x8_t a = __builtin_bit_cast(
           bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
@@ -918,7 +918,7 @@ __global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, 
   float l = l_run;
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
-  float* so = (float*)sV[wave];       // [SC][HD]: a wave's V rows hold SK * HD bf16
+  float* so = (float*)rows;       // [SC][HD]: a wave's V rows hold SK * HD bf16
   static_assert(SC * HD * 4 <= SK * ROWB, "a wave's output fits its V rows");
   if (c16 < cols) {
     if (g == 0) {
@@ -942,7 +942,7 @@ __global__ __launch_bounds__(256) void paged_step_kernel(int H, int col_groups, 
     for (int w = 0; w < 4; ++w) {
       // a wave without keys has l = 0 and o = 0: its factor does not matter
       const float f = s_m[w][j] == m ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][j] - m);
-      const f32x4_t v = *reinterpret_cast<const f32x4_t*>((const float*)sV[w] + j * HD + d);
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>((const float*)s_rows[w] + j * HD + d);
       ls = fmaf(f, s_l[w][j], ls);
 #pragma unroll
       for (int z = 0; z < 4; ++z) y[z] = fmaf(f, v[z], y[z]);
@@ -1005,7 +1005,7 @@ StepShape step_shape(const adept_paged_kv& kv, int n_heads, int max_active, int 
   const int G = n_heads / kv.n_kv_heads;
   t.groups = ceil_div(G, SC);
   const int64_t keys = (int64_t)max_pages * kv.page_size;
-  t.want = std::max(1, 8192 / (kv.n_kv_heads * t.groups));
+  t.want = std::max(1, kStepItems / (kv.n_kv_heads * t.groups));
   t.cut = keys > kStepUnit;
   const int64_t most = std::max<int64_t>(1, (keys + kStepUnit - 1) / kStepUnit);
   t.items = (int)std::min<int64_t>((int64_t)max_active + t.want, max_active * most);
