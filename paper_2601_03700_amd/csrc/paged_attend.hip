@@ -1,12 +1,12 @@
 // Attention of new tokens over a paged cache (adept_paged_attend).
 //
-// Tiles (bf16 queries, head_dim 64 / 128): the (entry, query head) pairs that
+// Tiles (head_dim 64 / 128): the (entry, query head) pairs that
 // read one K/V head of one sequence are the columns of a matrix; a plan kernel
 // cuts each sequence's columns into tiles of 128.  A workgroup takes one (tile,
 // K/V head) and, where there are too few of those to fill the card, a part of
 // the keys, which a second kernel joins.
 //
-// Walk (f32, other widths): one wave per (entry, head) takes the keys one after
+// Walk (other widths): one wave per (entry, head) takes the keys one after
 // another: lane l holds the dims l, l + 64, ... of q and of the running output,
 // a score is a sum over the wave.  A key that is not seen is skipped, whatever
 // it holds.
@@ -220,6 +220,17 @@ __device__ __forceinline__ float max_halves(float m) {
   const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return max3_raw(m, __uint_as_float(a[0]), __uint_as_float(a[1]));
 }
+__device__ __forceinline__ float max_column(float m) {   // over lanes l, l^16, l^32, l^48
+  const uint32_t u = __float_as_uint(m);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return max_halves(max3_raw(m, __uint_as_float(a[0]), __uint_as_float(a[1])));
+}
+__device__ __forceinline__ void store4(bf16* p, float a, float b, float c, float d) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+}
+__device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
+  *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
 __device__ __forceinline__ bool finite(float x) {
   return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
 }
@@ -229,6 +240,49 @@ __device__ __forceinline__ void column_of(const Tile& t, int j, int G, int hk, i
   const int c = t.col + j;
   *k = t.first + c / G;
   *h = hk * G + c % G;
+}
+
+// Work item of a workgroup, head by head: position in the order of the tiles
+// (-1: none), K/V head, part of the keys.  The hardware deals workgroups
+// round-robin to the 8 XCDs: with 8 K/V heads or more each XCD takes a run of
+// items, so that the tiles in flight on it share a few heads' K/V in its L2;
+// with fewer heads the items are dealt as they come, which keeps the XCDs evenly
+// loaded.
+struct TileItem {
+  int tile, head, part;
+  bool whole;      // takes all of its tile's keys
+};
+__device__ __forceinline__ TileItem tile_item(int max_tiles, int heads, int parts, int nt) {
+  const int total = max_tiles * heads * parts;
+  int item = blockIdx.x;
+  if (heads >= 8) {
+    const int per = (total + 7) >> 3;
+    item = (int)(blockIdx.x >> 3) < per ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : total;
+  }
+  TileItem t{item / parts % max_tiles, item / parts / max_tiles, item % parts, parts == 1};
+  // a list whose sequences are scattered can hold more tiles than the host
+  // counted on: then each workgroup takes several, with all of their keys
+  if (nt > max_tiles) t.whole = true;
+  if (item >= total || t.tile >= nt || (t.whole && t.part > 0)) t.tile = -1;
+  return t;
+}
+// The keys that some column of the tile sees: 0 .. result - 1.
+__device__ __forceinline__ int tile_end(const Entries& e, const PagedView& c, const Tile& tile, int G,
+                                        int hk) {
+  int n = 0;
+  for (int j = threadIdx.x & 63; j < tile.cols; j += 64) {
+    int k, h, b;
+    column_of(tile, j, G, hk, &k, &h);
+    n = max(n, entry_limit(e, c, e.rows[k], &b));
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n = max(n, __shfl_xor(n, o, 64));
+  return __builtin_amdgcn_readfirstlane(n);
+}
+__device__ __forceinline__ void part_keys(int n, int parts, int p, int* t0, int* t1) {
+  const int per = ((n + KB - 1) / KB + parts - 1) / parts * KB;
+  *t0 = min(p * per, n);
+  *t1 = min(*t0 + per, n);
 }
 
 // One workgroup per (tile, K/V head, part of the keys).  Wave w holds columns
@@ -269,68 +323,39 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
 
   const int G = H / c.n_kv_heads;
   const int nt = *n_tiles;
-  // Work items head by head.  The hardware deals workgroups round-robin to the
-  // 8 XCDs: with 8 K/V heads or more each XCD takes a run of items, so that the
-  // tiles in flight on it share a few heads' K/V in its L2; with fewer heads the
-  // items are dealt as they come, which keeps the XCDs evenly loaded.
-  const int total = max_tiles * c.n_kv_heads * parts;
-  int item = blockIdx.x;
-  if (c.n_kv_heads >= 8) {
-    const int per = (total + 7) >> 3;
-    item = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per) return;
-  }
-  if (item >= total) return;
-  const int p = item % parts, ti0 = item / parts % max_tiles, hk = item / parts / max_tiles;
-  // a list whose sequences are scattered can hold more tiles than the host
-  // counted on: then each workgroup takes several, with all of their keys
-  const bool whole = parts == 1 || nt > max_tiles;
-  if (whole && p > 0) return;
-
+  const TileItem it = tile_item(max_tiles, c.n_kv_heads, parts, nt);
+  if (it.tile < 0) return;
+  const int hk = it.head, p = it.part;
+  const bool whole = it.whole;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, c32 = lane & 31;
   auto fk = [](int r) { return HD == 128 ? (r & 15) : ((r >> 1) & 7); };
   auto fv = [](int r) { return HD == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
 
-  for (int ti = ti0; ti < nt; ti += max_tiles) {
+  for (int ti = it.tile; ti < nt; ti += max_tiles) {
     const Tile tile = tiles[nt - 1 - ti];   // of a prompt, the latest (longest) first
     const int32_t* pages = c.table + (int64_t)tile.seq * c.max_pages;
-    // keys that some column sees, this wave's columns, and this lane's column
-    int tend = 0, wend = 0, wfull = INT_MAX, qlim = 0;
-    for (int j = lane; j < tile.cols; j += 64) {
-      int k, h, b;
-      column_of(tile, j, G, hk, &k, &h);
-      tend = max(tend, entry_limit(e, c, e.rows[k], &b));
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) tend = max(tend, __shfl_xor(tend, o, 64));
-    tend = __builtin_amdgcn_readfirstlane(tend);
+    const int tend = tile_end(e, c, tile, G, hk);
     const int j = wave * 32 + c32;
     const bool valid = j < tile.cols;
-    int qk, qh;
+    int qk, qh, qlim = 0;
     column_of(tile, valid ? j : 0, G, hk, &qk, &qh);
     const int64_t qat = ((int64_t)qk * H + qh) * HD;
     if (valid) {
       int b;
       qlim = entry_limit(e, c, e.rows[qk], &b);
     }
-    wend = qlim;
-    wfull = valid ? qlim : INT_MAX;
+    int wend = qlim, wfull = valid ? qlim : INT_MAX;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       wend = max(wend, __shfl_xor(wend, o, 64));
       wfull = min(wfull, __shfl_xor(wfull, o, 64));
     }
-    wend = __builtin_amdgcn_readfirstlane(wend);
-    wfull = __builtin_amdgcn_readfirstlane(wfull);   // keys below it: every column sees them
-    // this part's keys
-    int tb = 0, te = tend;
-    if (!whole) {
-      const int per = ((tend + KB - 1) / KB + parts - 1) / parts * KB;
-      tb = min(p * per, tend);
-      te = min(tb + per, tend);
-    }
+    wend = __builtin_amdgcn_readfirstlane(wend);     // the wave's columns see keys below it,
+    wfull = __builtin_amdgcn_readfirstlane(wfull);   // and all of them the ones below this
+    int tb, te;
+    part_keys(tend, whole ? 1 : parts, p, &tb, &te);
     const int nkb = (te - tb + KB - 1) / KB;
 
     bf16x8_t qf[DS];
@@ -575,11 +600,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
 }
 
 // Joins the parts of each (tile, K/V head): a thread takes four dims of a column.
-template <int HD>
+template <typename T, int HD>
 __global__ __launch_bounds__(256) void paged_tile_join_kernel(
-    int H, Entries e, int n_kv_heads, const Tile* __restrict__ tiles,
+    int H, int n_kv_heads, const Tile* __restrict__ tiles,
     const int32_t* __restrict__ n_tiles, int max_tiles, int parts, const float* __restrict__ part,
-    bf16* __restrict__ out) {
+    T* __restrict__ out) {
   constexpr int CPB = 256 / (HD / 4);      // columns of a workgroup
   const int ti = blockIdx.x, hk = blockIdx.y, nt = *n_tiles;
   if (ti >= nt || nt > max_tiles) return;
@@ -606,8 +631,235 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   int k, h;
   column_of(tile, j, G, hk, &k, &h);
-  *reinterpret_cast<uint2*>(out + ((int64_t)k * H + h) * HD + d) =
-      make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+  store4(out + ((int64_t)k * H + h) * HD + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+}
+
+// ---------------------------------------------------------------------------
+// tiles of f32 queries
+// ---------------------------------------------------------------------------
+constexpr int kTile32Threads = 512;
+constexpr int KB32 = 32;
+
+// As paged_tile_kernel, in f32 throughout (v_mfma_f32_16x16x4_f32): eight waves of
+// 16 columns, blocks of 32 keys in one stage of LDS, the next block's rows in
+// registers while a block is computed.  A score tile is 16 keys x 16 columns;
+// lane (g, c) holds the keys 4 g + 0 .. 3 of column c, so product v of
+// O^T += V^T P^T takes the keys 4 g + v from its register v as they are.  Bound by
+// the f32 matrix rate (1/16 of bf16's), small calls by their launches.
+template <int HD, bool FP8>
+__global__ __launch_bounds__(kTile32Threads) void paged_tile_f32_kernel(
+    int H, float scale_log2, const float* __restrict__ q, Entries e, PagedView c,
+    const Tile* __restrict__ tiles, const int32_t* __restrict__ n_tiles, int max_tiles, int parts,
+    float* __restrict__ out, float* __restrict__ part) {
+  constexpr int DB = HD / 16;
+  constexpr int ROW = HD;                            // floats of a row in LDS
+  constexpr int NCH = HD * (FP8 ? 1 : 4) / 16;       // 16-byte pieces of a cache row
+  constexpr int PPT = (KB32 * NCH + kTile32Threads - 1) / kTile32Threads;   // of a thread
+  __shared__ __attribute__((aligned(16))) float sKV[2][KB32 * ROW];
+  const int G = H / c.n_kv_heads;
+  const int nt = *n_tiles;
+  const TileItem it = tile_item(max_tiles, c.n_kv_heads, parts, nt);
+  if (it.tile < 0) return;
+  const int hk = it.head, p = it.part;
+  const bool whole = it.whole;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, c16 = lane & 15;
+  // 16-byte chunk ch of row r lies at ch ^ f(r): the reads of K (16 rows, a
+  // chunk) and of V (4 rows four apart, 64 bytes) fall on distinct banks
+  auto fk = [](int r) { return r & 15; };
+  auto fv = [](int r) { return 4 * ((r >> 2) & 3); };
+
+  for (int ti = it.tile; ti < nt; ti += max_tiles) {
+    const Tile tile = tiles[nt - 1 - ti];
+    const int32_t* pages = c.table + (int64_t)tile.seq * c.max_pages;
+    const int tend = tile_end(e, c, tile, G, hk);
+    const int j = wave * 16 + c16;
+    const bool valid = j < tile.cols;
+    int qk, qh, qlim = 0;
+    column_of(tile, valid ? j : 0, G, hk, &qk, &qh);
+    const int64_t qat = ((int64_t)qk * H + qh) * HD;
+    if (valid) {
+      int b;
+      qlim = entry_limit(e, c, e.rows[qk], &b);
+    }
+    int wend = qlim;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) wend = max(wend, __shfl_xor(wend, o, 64));
+    wend = __builtin_amdgcn_readfirstlane(wend);
+    int tb, te;
+    part_keys(tend, whole ? 1 : parts, p, &tb, &te);
+    const int nkb = (te - tb + KB32 - 1) / KB32;
+
+    f32x4_t qf[HD / 16];      // dims 16 i + 4 g + 0 .. 3
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i)
+      qf[i] = *reinterpret_cast<const f32x4_t*>(q + qat + i * 16 + g * 4);
+    f32x4_t o[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_ref = -INFINITY, l_run = 0.0f;
+
+    auto key_of = [&](int kb) { return tb + kb * KB32 + (lane & 31); };
+    auto page_of = [&](int kb) { return pages[min(key_of(kb), te - 1) >> c.shift]; };
+    const int64_t rowc = (int64_t)c.n_kv_heads * HD;
+    u32x4_t x[2][PPT];
+    uint8_t xs[2][PPT];
+    uint32_t there = 0;
+    // rows of keys that are not there: slot 0's, cleared on their way to LDS
+    auto fetch = [&](int kb, int page) {
+      const int sl = c.slot(page, key_of(kb), key_of(kb) < te);
+      there = (uint32_t)__ballot(sl >= 0);
+#pragma unroll
+      for (int i = 0; i < PPT; ++i) {
+        const int pc = i * kTile32Threads + tid, r = pc / NCH % KB32;
+        const int s = max(__shfl(sl, r, 64), 0);
+#pragma unroll
+        for (int op = 0; op < 2; ++op) {
+          const char* src = (const char*)(op ? c.v : c.k) + (s * rowc + hk * HD) * (FP8 ? 1 : 4);
+          x[op][i] = *reinterpret_cast<const u32x4_t*>(src + pc % NCH * 16);
+          if constexpr (FP8)
+            xs[op][i] = (op ? c.v_scale : c.k_scale)[(int64_t)s * c.n_kv_heads + hk];
+        }
+      }
+    };
+    auto put = [&]() {
+#pragma unroll
+      for (int i = 0; i < PPT; ++i) {
+        const int pc = i * kTile32Threads + tid, r = pc / NCH, ch = pc % NCH;
+        if (r >= KB32) continue;
+        const bool in = (there >> r) & 1;
+#pragma unroll
+        for (int op = 0; op < 2; ++op) {
+          float* row = sKV[op] + r * ROW;
+          const int f = op ? fv(r) : fk(r);
+          if constexpr (FP8) {
+            const float sc = scale_of(xs[op][i]);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+              const float2 a = fp8x2_to_f32x2<false>(x[op][i][z], sc);
+              const float2 b = fp8x2_to_f32x2<true>(x[op][i][z], sc);
+              const f32x4_t y = in ? f32x4_t{a.x, a.y, b.x, b.y} : f32x4_t{0.f, 0.f, 0.f, 0.f};
+              *reinterpret_cast<f32x4_t*>(row + ((4 * ch + z) ^ f) * 4) = y;
+            }
+          } else {
+            *reinterpret_cast<u32x4_t*>(row + (ch ^ f) * 4) = in ? x[op][i] : u32x4_t{0, 0, 0, 0};
+          }
+        }
+      }
+    };
+    int page = 0;
+    if (nkb > 0) {
+      page = page_of(0);
+      fetch(0, page);
+      page = page_of(1);
+    }
+    for (int kb = 0; kb < nkb; ++kb) {
+      const int t0 = tb + kb * KB32;
+      const uint32_t mask = there;
+      put();
+      __syncthreads();
+      if (kb + 1 < nkb) {
+        const int next = page;
+        page = page_of(kb + 2);
+        fetch(kb + 1, next);
+      }
+      if (t0 < wend) {
+        f32x4_t s[2];
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb) {
+          s[sb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          const int r = sb * 16 + c16;
+#pragma unroll
+          for (int i = 0; i < HD / 16; ++i) {
+            const f32x4_t a =
+                *reinterpret_cast<const f32x4_t*>(sKV[0] + r * ROW + ((4 * i + g) ^ fk(r)) * 4);
+#pragma unroll
+            for (int z = 0; z < 4; ++z)
+              s[sb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[z], qf[i][z], s[sb], 0, 0, 0);
+          }
+        }
+        float mb = -INFINITY;
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int kl = sb * 16 + 4 * g + v;
+            s[sb][v] = t0 + kl < qlim && ((mask >> kl) & 1) ? s[sb][v] * scale_log2 : -INFINITY;
+            mb = max3_raw(mb, s[sb][v], s[sb][v]);
+          }
+        mb = max_column(mb);
+        const float mn = fmaxf(m_ref, mb);
+        const float alpha = mn == m_ref ? 1.0f : __builtin_amdgcn_exp2f(m_ref - mn);
+        const float msub = mn == -INFINITY ? 0.0f : mn;
+        m_ref = mn;
+        l_run *= alpha;
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) o[i][v] *= alpha;
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            s[sb][v] = __builtin_amdgcn_exp2f(s[sb][v] - msub);
+            l_run += s[sb][v];
+          }
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int r = sb * 16 + 4 * g + v;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              const float a = sKV[1][r * ROW + (((4 * db + (c16 >> 2)) ^ fv(r)) * 4) + (c16 & 3)];
+              o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[sb][v], o[db], 0, 0, 0);
+            }
+          }
+      }
+      __syncthreads();
+    }
+    float l = l_run;
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    bool ok = finite(l);
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) ok &= finite(o[i][v]);
+    uint64_t bad = __ballot(valid && !ok);
+    bad |= bad >> 32;
+    const uint32_t redo = (uint32_t)(bad | (bad >> 16)) & 0xffffu;
+    float* pp = nullptr;
+    if (!whole) pp = part + (((int64_t)(nt - 1 - ti) * c.n_kv_heads + hk) * parts + p) * TC_ * (HD + 2);
+    if (valid && !((redo >> c16) & 1)) {
+      const float f = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+      float* dst = whole ? out + qat : pp + TC_ * 2 + j * HD;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        f32x4_t y = o[db];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y[v] *= f;
+        *reinterpret_cast<f32x4_t*>(dst + db * 16 + g * 4) = y;
+      }
+      if (!whole && g == 0) *reinterpret_cast<float2*>(pp + 2 * j) = make_float2(m_ref, l);
+    }
+    for (uint32_t left = redo; left; left &= left - 1) {
+      const int y = __ffs(left) - 1, jj = wave * 16 + y;
+      int k, h;
+      column_of(tile, jj, G, hk, &k, &h);
+      const int lim = min(__shfl(qlim, y, 64), te);
+      const int64_t at = ((int64_t)k * H + h) * HD;
+      const auto w = walk_keys<float, typename std::conditional<FP8, uint8_t, float>::type, HD / 64>(
+          q + at, HD, scale_log2, c, pages, hk, tb, lim);
+      if (whole) {
+        walk_store(w, HD, out + at);
+      } else {
+        for (int i = 0; i < HD / 64; ++i) pp[TC_ * 2 + jj * HD + lane + 64 * i] = w.o[i];
+        if (lane == 0) *reinterpret_cast<float2*>(pp + 2 * jj) = make_float2(w.m, w.l);
+      }
+    }
+  }
 }
 
 // Tiles that the host counts on, and the parts of the keys with which they make
@@ -635,9 +887,7 @@ TileShape tile_shape(const adept_paged_kv& kv, int n_heads, int max_active, int 
   return t;
 }
 
-bool tiles_fit(adept_dtype dt, const adept_paged_kv& kv) {
-  return dt == ADEPT_BF16 && (kv.head_dim == 64 || kv.head_dim == 128);
-}
+bool tiles_fit(const adept_paged_kv& kv) { return kv.head_dim == 64 || kv.head_dim == 128; }
 
 // ---------------------------------------------------------------------------
 // steps: one entry per sequence
@@ -650,12 +900,6 @@ constexpr int SC = 16;             // columns
 // 119 us with 2048, 131 with 4096, 153 with 8192 (a workgroup starts with some
 // five dependent loads); 64 sequences of 4096 keys, 32 heads, 653, 641 and 663 us.
 constexpr int kStepItems = 2048;
-
-__device__ __forceinline__ float max_column(float m) {   // over lanes l, l^16, l^32, l^48
-  const uint32_t u = __float_as_uint(m);
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  return max_halves(max3_raw(m, __uint_as_float(a[0]), __uint_as_float(a[1])));
-}
 
 // Item x of the call: a stretch of one entry's keys.  Every workgroup finds its
 // own: entries of all workgroups' keys together, cut into about `want` stretches
@@ -1019,7 +1263,7 @@ StepShape step_shape(const adept_paged_kv& kv, int n_heads, int max_active, int 
 }
 // one entry per sequence at most, on average: each reads its keys for itself
 bool step_fits(adept_dtype dt, const adept_paged_kv& kv, int max_active, int n_seq) {
-  return tiles_fit(dt, kv) && max_active <= n_seq;
+  return dt == ADEPT_BF16 && tiles_fit(kv) && max_active <= n_seq;
 }
 
 }  // namespace
@@ -1098,7 +1342,7 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
     }
     return launch_status("paged_attend");
   }
-  if (tiles_fit(dt, *kv)) {
+  if (tiles_fit(*kv)) {
     const TileShape ts = tile_shape(*kv, n_heads, max_active, n_seq, max_pages);
     char* w = (char*)workspace;
     int32_t* n_tiles = (int32_t*)w;
@@ -1109,25 +1353,36 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
     ADEPT_LAUNCH(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, e, n_heads / kv->n_kv_heads,
                  (int32_t*)(w + ts.off_starts), tiles, n_tiles);
     ADEPT_CHECK_LAUNCH("paged_plan");
-#define ADEPT_TILE(HD, FP8)                                                                      \
-  ADEPT_LAUNCH((paged_tile_kernel<HD, FP8>), dim3((unsigned)((items + 7) / 8 * 8)),              \
-               dim3(kTileThreads), 0, s, n_heads, sl, (const bf16*)q, e, c, tiles, n_tiles,      \
-               ts.max_tiles, ts.parts, (bf16*)out, part)
-    if (hd == 128) {
-      if (fp8) ADEPT_TILE(128, true); else ADEPT_TILE(128, false);
-    } else {
-      if (fp8) ADEPT_TILE(64, true); else ADEPT_TILE(64, false);
-    }
+    const dim3 grid((unsigned)((items + 7) / 8 * 8));
+#define ADEPT_TILE(KERNEL, T, HD, FP8, THREADS)                                                  \
+  ADEPT_LAUNCH((KERNEL<HD, FP8>), grid, dim3(THREADS), 0, s, n_heads, sl, (const T*)q, e, c,     \
+               tiles, n_tiles, ts.max_tiles, ts.parts, (T*)out, part)
+#define ADEPT_TILES(KERNEL, T, THREADS)                                                          \
+  do {                                                                                           \
+    if (hd == 128) {                                                                             \
+      if (fp8) ADEPT_TILE(KERNEL, T, 128, true, THREADS);                                        \
+      else ADEPT_TILE(KERNEL, T, 128, false, THREADS);                                           \
+    } else {                                                                                     \
+      if (fp8) ADEPT_TILE(KERNEL, T, 64, true, THREADS);                                         \
+      else ADEPT_TILE(KERNEL, T, 64, false, THREADS);                                            \
+    }                                                                                            \
+  } while (0)
+    if (dt == ADEPT_BF16) ADEPT_TILES(paged_tile_kernel, bf16, kTileThreads);
+    else ADEPT_TILES(paged_tile_f32_kernel, float, kTile32Threads);
+#undef ADEPT_TILES
 #undef ADEPT_TILE
     ADEPT_CHECK_LAUNCH("paged_tile");
     if (ts.parts > 1) {
       const dim3 jg(ts.max_tiles, kv->n_kv_heads, TC_ * hd / 1024);
-      if (hd == 128)
-        ADEPT_LAUNCH(paged_tile_join_kernel<128>, jg, dim3(256), 0, s, n_heads, e, kv->n_kv_heads,
-                     tiles, n_tiles, ts.max_tiles, ts.parts, part, (bf16*)out);
-      else
-        ADEPT_LAUNCH(paged_tile_join_kernel<64>, jg, dim3(256), 0, s, n_heads, e, kv->n_kv_heads,
-                     tiles, n_tiles, ts.max_tiles, ts.parts, part, (bf16*)out);
+#define ADEPT_JOIN(T, HD)                                                                        \
+  ADEPT_LAUNCH((paged_tile_join_kernel<T, HD>), jg, dim3(256), 0, s, n_heads, kv->n_kv_heads,    \
+               tiles, n_tiles, ts.max_tiles, ts.parts, part, (T*)out)
+      if (dt == ADEPT_BF16) {
+        if (hd == 128) ADEPT_JOIN(bf16, 128); else ADEPT_JOIN(bf16, 64);
+      } else {
+        if (hd == 128) ADEPT_JOIN(float, 128); else ADEPT_JOIN(float, 64);
+      }
+#undef ADEPT_JOIN
     }
     return launch_status("paged_attend");
   }
