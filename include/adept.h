@@ -25,7 +25,7 @@
  *  - Element types: ADEPT_F32 (float) or ADEPT_BF16 (bfloat16 stored as
  *    uint16).  Inertia is always float, similarities double.
  *  - Caches K and V are [N][n_slots][H][hd]; a token's slot is
- *    b * s_max + p (sequence b, position p).
+ *    b * s_max + p (sequence b, position p), or one in its pages (below).
  */
 #ifndef ADEPT_H
 #define ADEPT_H
@@ -347,8 +347,8 @@ adept_status adept_attend(adept_dtype dt, int n_heads, int head_dim, float scale
  * the bit.  Reading back is exact in either source type (4 significant bits).
  *
  * page_size is a power of two (1 .. 1024), head_dim a power of two (16 .. 256),
- * n_pages * page_size below 2^31 - 1023; k, v and the scales 16-byte aligned.  A call
- * takes at most 2^23 rows or entries.
+ * n_pages * page_size below 2^31 - 1023; k and v 16-byte aligned.  A call takes at
+ * most 2^23 rows or entries.
  * ------------------------------------------------------------------------- */
 typedef enum { ADEPT_KV_F32 = 0, ADEPT_KV_BF16 = 1, ADEPT_KV_FP8 = 2 } adept_kv_dtype;
 
@@ -505,6 +505,25 @@ typedef struct {
 
 size_t adept_layer_workspace_bytes(const adept_layer_args* a);
 adept_status adept_layer_step(const adept_layer_args* a, int layer, void* stream);
+
+/* adept_layer_step over a paged cache: a prompt in pieces (attn_tiles = 1; each
+ * piece attends over the ones before) or a decode pass (0).
+ *
+ *  kv describes layer 1, the other layers lie behind it: k, v [N][n_pages*page_size][H][hd], scales
+ *  [N][n_pages*page_size][H]; page_table, max_pages as for adept_paged_attend.
+ *  a->s_max is not used.  F32 / BF16 cache: a->k_cache, a->v_cache and
+ *  a->n_slots are the same cache, a->slot[j] row j's slot in it.  FP8 cache:
+ *  the GEMMs write K and V into a->k_cache, a->v_cache [N][n_slots][H][hd] (dtype,
+ *  n_slots >= n_tok, 16-byte aligned) with a->slot[j] = j, and each step
+ *  quantises its layer's rows of the whole pass into their slots cache_slot[j]
+ *  (-1 for a row that is no part of the pass) before it attends; a decode pass
+ *  then needs kv_fused (or attn_tiles = 1).
+ *  workspace: adept_layer_paged_workspace_bytes(a, kv, max_pages). */
+size_t adept_layer_paged_workspace_bytes(const adept_layer_args* a, const adept_paged_kv* kv,
+                                         int max_pages);
+adept_status adept_layer_step_paged(const adept_layer_args* a, const adept_paged_kv* kv,
+                                    const int32_t* page_table, int max_pages,
+                                    const int32_t* cache_slot, int layer, void* stream);
 
 /* Folds a norm gain into the weight matrices that consume the normalised
  * vector, in place: w[l][o][c] *= gain[l][c] for l < n_mats, o < rows,

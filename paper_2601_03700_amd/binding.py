@@ -126,6 +126,10 @@ _SIGS = {
                                   _sz, _vp]),
     "adept_layer_workspace_bytes": (_sz, [ctypes.POINTER(LayerArgs)]),
     "adept_layer_step": (_i32, [ctypes.POINTER(LayerArgs), _i32, _vp]),
+    "adept_layer_paged_workspace_bytes": (_sz, [ctypes.POINTER(LayerArgs), ctypes.POINTER(PagedKv),
+                                               _i32]),
+    "adept_layer_step_paged": (_i32, [ctypes.POINTER(LayerArgs), ctypes.POINTER(PagedKv), _vp, _i32,
+                                      _vp, _i32, _vp]),
     "adept_embed": (_i32, [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
     "adept_final_logits": (_i32, [_i32, _i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _vp,
                                   _i32, _vp, _vp, _vp, _vp, _vp]),
@@ -490,6 +494,17 @@ def layer_workspace_bytes(args: LayerArgs):
 def layer_step(args: LayerArgs, layer, stream=None):
     _check(lib().adept_layer_step(ctypes.byref(args), layer, stream_handle(stream)),
            "adept_layer_step")
+
+
+def layer_paged_workspace_bytes(args: LayerArgs, kv, max_pages):
+    return lib().adept_layer_paged_workspace_bytes(ctypes.byref(args), ctypes.byref(kv), max_pages)
+
+
+def layer_step_paged(args: LayerArgs, kv, page_table, layer, cache_slot=None, stream=None):
+    """layer_step over a paged cache; kv: paged_kv of its first layer, the others behind it."""
+    _check(lib().adept_layer_step_paged(ctypes.byref(args), ctypes.byref(kv), ptr(page_table),
+                                        page_table.shape[1], ptr(cache_slot), layer,
+                                        stream_handle(stream)), "adept_layer_step_paged")
 
 
 def embed(n, d_model, vocab, ids, table, h0, stream=None):

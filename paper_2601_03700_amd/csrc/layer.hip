@@ -16,10 +16,19 @@
 //    its row count, so the generation costs no weight traffic.
 #include <algorithm>
 
-#include "common.h"
+#include "paged.h"
 
 namespace adept {
 namespace {
+
+// The paged cache of a step (adept_layer_step_paged), all layers; NULL: the
+// contiguous one of the arguments.
+struct PagedStep {
+  const adept_paged_kv* kv;
+  const int32_t* table;
+  int max_pages;
+  const int32_t* cache_slot;   // FP8: slots of the rows, whose K/V the GEMMs write to a->k_cache
+};
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -51,7 +60,7 @@ bool step_direct(const adept_layer_args* a) {
          gemm_direct_fits(n, D, F, EPI_RESID);
 }
 
-LayerWs carve(const adept_layer_args* a, void* base) {
+LayerWs carve(const adept_layer_args* a, void* base, const PagedStep* pg) {
   LayerWs w{};
   char* p = (char*)base;
   size_t off = 0;
@@ -59,7 +68,9 @@ LayerWs carve(const adept_layer_args* a, void* base) {
   w.rinv = (float*)(p + off); off += align256((size_t)a->n_tok * sizeof(float));
   w.compact_bytes = adept_compact_workspace_bytes(a->n_tok);
   w.compact = p + off; off += align256(w.compact_bytes);
-  w.attend_bytes = attend_workspace_bytes(a->n_tok, a->n_seq, a->n_heads, a->head_dim, a->s_max);
+  w.attend_bytes = pg ? adept_paged_attend_workspace_bytes(pg->kv, a->n_heads, a->n_tok, a->n_seq,
+                                                           pg->max_pages)
+                      : attend_workspace_bytes(a->n_tok, a->n_seq, a->n_heads, a->head_dim, a->s_max);
   w.attend = p + off; off += align256(w.attend_bytes);
   const bool gpt2 = a->family == ADEPT_FAMILY_GPT2;
   w.kvgen_bytes = gpt2 ? adept_kv_generate_layernorm_workspace_bytes(a->n_layers, a->n_tok,
@@ -255,6 +266,40 @@ adept_status kv_generate_family(const adept_layer_args* a, int max_skipped, adep
                           ws.kvgen_bytes, stream);
 }
 
+// Step 3: attention over the mixed cache.  Over an FP8 cache the layer's K/V of
+// all rows of the pass are quantised into their slots first: those of the active
+// rows the QKV GEMM has just written, those of the rows that exited before were
+// generated after their exit or by that GEMM.
+adept_status attend_step(const adept_layer_args* a, const PagedStep* pg, int layer, const void* kc,
+                         const void* vc, const int32_t* act, const int32_t* nact,
+                         const LayerWs& ws, hipStream_t s) {
+  const adept_dtype dt = (adept_dtype)a->dtype;
+  const int H = a->n_heads, hd = a->head_dim, dq = H * hd;
+  const float scale = 1.0f / sqrtf((float)hd);
+  if (!pg)
+    return attend_dispatch(dt, H, hd, scale, 1, a->q_buf, act, nact, a->max_active, a->pos, a->seq,
+                           a->n_seq, kc, vc, a->s_max, nullptr, nullptr, a->attn_out, ws.attend,
+                           ws.attend_bytes, a->attn_tiles != 0, s);
+  adept_paged_kv kv = *pg->kv;
+  const int64_t slots = (int64_t)(layer - 1) * paged_slots(kv);
+  if (kv.dtype == ADEPT_KV_FP8) {
+    kv.k = (uint8_t*)kv.k + slots * dq;
+    kv.v = (uint8_t*)kv.v + slots * dq;
+    kv.k_scale += slots * H;
+    kv.v_scale += slots * H;
+    ADEPT_TRY(adept_paged_store(dt, &kv, kc, dq, vc, dq, nullptr, nullptr, a->n_tok, pg->cache_slot,
+                                s));
+  } else {
+    kv.k = (void*)kc;
+    kv.v = (void*)vc;
+  }
+  return adept_paged_attend(dt, &kv, H, scale, 1, a->q_buf, act, nact, a->max_active, a->pos, a->seq,
+                            a->n_seq, pg->table, pg->max_pages, nullptr, nullptr, a->attn_out,
+                            ws.attend, ws.attend_bytes, s);
+}
+
+adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* pg, void* stream);
+
 }  // namespace
 }  // namespace adept
 
@@ -262,11 +307,50 @@ using namespace adept;
 
 extern "C" size_t adept_layer_workspace_bytes(const adept_layer_args* a) {
   if (!a) return 0;
-  return carve(a, nullptr).total;
+  return carve(a, nullptr, nullptr).total;
+}
+
+extern "C" size_t adept_layer_paged_workspace_bytes(const adept_layer_args* a,
+                                                    const adept_paged_kv* kv, int max_pages) {
+  if (!a || !kv) return 0;
+  const PagedStep pg{kv, nullptr, max_pages, nullptr};
+  return carve(a, nullptr, &pg).total;
 }
 
 extern "C" adept_status adept_layer_step(const adept_layer_args* a, int layer, void* stream) {
   ADEPT_REQUIRE(a != nullptr, "layer_step: args is NULL");
+  return layer_step(a, layer, nullptr, stream);
+}
+
+extern "C" adept_status adept_layer_step_paged(const adept_layer_args* a, const adept_paged_kv* kv,
+                                               const int32_t* page_table, int max_pages,
+                                               const int32_t* cache_slot, int layer, void* stream) {
+  ADEPT_REQUIRE(a != nullptr, "layer_step_paged: args is NULL");
+  ADEPT_TRY(paged_check("layer_step_paged", (adept_dtype)a->dtype, kv));
+  ADEPT_REQUIRE(kv->n_kv_heads == a->n_heads && kv->head_dim == a->head_dim,
+                "layer_step_paged: the cache's heads are not the layer's");
+  ADEPT_REQUIRE(a->n_layers >= 1 && a->n_tok <= kMaxEntries && a->n_seq > 0, "layer_step_paged: bad sizes");
+  ADEPT_REQUIRE(page_table && max_pages > 0 && (int64_t)max_pages * kv->page_size <= kMaxTokens,
+                "layer_step_paged: bad page table");
+  if (kv->dtype == ADEPT_KV_FP8) {
+    ADEPT_REQUIRE(cache_slot != nullptr, "layer_step_paged: an FP8 cache needs the rows' slots");
+    ADEPT_REQUIRE(a->n_slots >= a->n_tok, "layer_step_paged: fewer K/V rows than rows of the pass");
+    ADEPT_REQUIRE(aligned16(a->k_cache) && aligned16(a->v_cache),
+                  "layer_step_paged: the K/V rows must be 16-byte aligned");
+    // generated after layer N, the K/V of exited rows would miss their slots
+    ADEPT_REQUIRE(a->attn_tiles || a->kv_fused,
+                  "layer_step_paged: a decode pass over an FP8 cache needs kv_fused");
+  } else {
+    ADEPT_REQUIRE(a->k_cache == kv->k && a->v_cache == kv->v && a->n_slots == paged_slots(*kv),
+                  "layer_step_paged: the arguments' cache is not the paged one");
+  }
+  const PagedStep pg{kv, page_table, max_pages, cache_slot};
+  return layer_step(a, layer, &pg, stream);
+}
+
+namespace adept {
+namespace {
+adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* pg, void* stream) {
   const adept_dtype dt = (adept_dtype)a->dtype;
   ADEPT_REQUIRE(dt == ADEPT_F32 || dt == ADEPT_BF16, "layer_step: bad dtype");
   const int N = a->n_layers, D = a->d_model, H = a->n_heads, hd = a->head_dim, F = a->d_ff;
@@ -274,7 +358,8 @@ extern "C" adept_status adept_layer_step(const adept_layer_args* a, int layer, v
   ADEPT_REQUIRE(a->exit.n_layers == N, "layer_step: exit.n_layers != n_layers");
   ADEPT_REQUIRE(D > 0 && H > 0 && hd > 0 && F > 0 && a->n_tok > 0, "layer_step: bad sizes");
   ADEPT_REQUIRE(a->max_active >= 0 && a->max_active <= a->n_tok, "layer_step: bad max_active");
-  ADEPT_REQUIRE(a->n_seq > 0 && a->s_max > 0 && a->n_slots >= (int64_t)a->n_seq * a->s_max,
+  ADEPT_REQUIRE(pg || (a->n_seq > 0 && a->s_max > 0 &&
+                       a->n_slots >= (int64_t)a->n_seq * a->s_max),
                 "layer_step: cache smaller than n_seq * s_max");
   const bool gpt2 = a->family == ADEPT_FAMILY_GPT2;
   ADEPT_REQUIRE(a->family == ADEPT_FAMILY_LLAMA || gpt2, "layer_step: bad family %d", a->family);
@@ -295,12 +380,12 @@ extern "C" adept_status adept_layer_step(const adept_layer_args* a, int layer, v
                 "layer_step: GLOBAL/BOTH metrics need inertia");
   ADEPT_REQUIRE(!a->hsm || (dt == ADEPT_BF16 && a->exit.metric != ADEPT_SIM_LOCAL && a->inertia),
                 "layer_step: the mapper needs bf16 and the inertia (GLOBAL or BOTH metric)");
-  const size_t need = adept_layer_workspace_bytes(a);
+  const size_t need = carve(a, nullptr, pg).total;
   if (!a->workspace || a->workspace_bytes < need) {
     set_error("layer_step: workspace of %zu bytes needed", need);
     return ADEPT_E_WORKSPACE;
   }
-  LayerWs ws = carve(a, a->workspace);
+  LayerWs ws = carve(a, a->workspace, pg);
   hipStream_t s = as_stream(stream);
   const int in = (layer - 1) & 1, out = layer & 1;
   const int32_t* act = a->active[in];
@@ -410,9 +495,7 @@ extern "C" adept_status adept_layer_step(const adept_layer_args* a, int layer, v
     if (tail) g.list = &list;
     ADEPT_TRY(gemm(dt, g, s));
     // 3. attention over the mixed cache
-    ADEPT_TRY(attend_dispatch(dt, H, hd, 1.0f / sqrtf((float)hd), 1, a->q_buf, act, nact, maxn,
-                              a->pos, a->seq, a->n_seq, kc, vc, a->s_max, nullptr, nullptr,
-                              a->attn_out, ws.attend, ws.attend_bytes, a->attn_tiles != 0, s));
+    ADEPT_TRY(attend_step(a, pg, layer, kc, vc, act, nact, ws, s));
     // 4. output projection + bias + residual: h[out] = h[in] + o Wo^T + bo
     GemmArgs go{};
     go.M_max = maxn; go.M_dev = nact; go.N = D; go.K = dq;
@@ -482,9 +565,7 @@ extern "C" adept_status adept_layer_step(const adept_layer_args* a, int layer, v
                              qrows, nq, qmax, ws.rinv, s));
     ADEPT_TRY(run_gemm(dt, g, ws.gemm_tmp, s));
     // 3. attention over the mixed cache
-    ADEPT_TRY(attend_dispatch(dt, H, hd, 1.0f / sqrtf((float)hd), 1, a->q_buf, act, nact, maxn,
-                              a->pos, a->seq, a->n_seq, kc, vc, a->s_max, nullptr, nullptr,
-                              a->attn_out, ws.attend, ws.attend_bytes, a->attn_tiles != 0, s));
+    ADEPT_TRY(attend_step(a, pg, layer, kc, vc, act, nact, ws, s));
     // 4. output projection + residual: h[out] = h[in] + o Wo^T
     GemmArgs go{};
     go.M_max = maxn; go.M_dev = nact; go.N = D; go.K = dq;
@@ -570,3 +651,5 @@ extern "C" adept_status adept_layer_step(const adept_layer_args* a, int layer, v
   }
   return ADEPT_OK;
 }
+}  // namespace
+}  // namespace adept

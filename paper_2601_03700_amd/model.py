@@ -13,6 +13,11 @@ in place of the embedding gather and the RMSNorm head).
 A prefill runs the rows of a [B, T] prompt batch (row b*T + p); a decode
 step runs one new token per sequence against the cache the prefill (and
 earlier steps) filled, with generated entries for every skipped layer.
+
+The cache is either a KVCache (s_max slots for each sequence) or a
+PagedKVCache: pages that sequences take as they grow and give back, in the
+model's type or in 8 bits.  Over either, a prompt can be run in pieces
+(prefill with start).
 """
 from __future__ import annotations
 
@@ -40,6 +45,81 @@ class KVCache:
         return self.n_seq * self.s_max
 
 
+class PagedKVCache:
+    """The K/V cache of n_seq sequences in n_pages pages of page_size token slots per layer
+    (k, v [N, n_pages * page_size, H, hd]), each sequence up to max_pages of them; kv_dtype:
+    "f32", "bf16" or "fp8" (e4m3 codes with a scale byte per slot and head, k_scale, v_scale).
+    page_table [n_seq, max_pages] int32 on the device (-1: no page); which pages are free is
+    known on the host."""
+
+    def __init__(self, n_layers, n_heads, head_dim, n_seq, n_pages, page_size, max_pages, kv_dtype,
+                 device):
+        dims = (n_layers, n_pages * page_size, n_heads, head_dim)
+        tdt = torch.uint8 if kv_dtype == "fp8" else _TORCH_DT[kv_dtype]
+        self.k = torch.empty(dims, dtype=tdt, device=device)
+        self.v = torch.empty(dims, dtype=tdt, device=device)
+        self.k_scale = self.v_scale = None
+        if kv_dtype == "fp8":
+            self.k_scale = torch.empty(dims[:3], dtype=torch.uint8, device=device)
+            self.v_scale = torch.empty(dims[:3], dtype=torch.uint8, device=device)
+        self.kv_dtype, self.n_seq, self.page_size, self.max_pages = (kv_dtype, n_seq, page_size,
+                                                                     max_pages)
+        self.page_table = torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=device)
+        self._free = list(range(n_pages - 1, -1, -1))
+        self._pages = [[] for _ in range(n_seq)]
+        self.kv = self.layer_kv(1)
+
+    @property
+    def n_slots(self):
+        return self.k.shape[1]
+
+    @property
+    def s_max(self):
+        return self.max_pages * self.page_size
+
+    @property
+    def free_pages(self):
+        return len(self._free)
+
+    def layer_kv(self, layer):
+        """Descriptor of one layer (binding.paged_kv), for the operators of a single layer."""
+        i = layer - 1
+        scales = (None, None) if self.k_scale is None else (self.k_scale[i], self.v_scale[i])
+        return B.paged_kv(self.k[i], self.v[i], self.page_size, *scales)
+
+    def reserve(self, lengths):
+        """Pages for lengths[b] tokens of sequence b (a dict or one number for all); raises
+        ValueError, with nothing taken, where they do not fit."""
+        if not isinstance(lengths, dict):
+            lengths = {b: int(lengths) for b in range(self.n_seq)}
+        more = {b: -(-n // self.page_size) - len(self._pages[b]) for b, n in lengths.items()}
+        for b, n in lengths.items():
+            if not 0 <= n <= self.s_max:
+                raise ValueError(f"{n} tokens of sequence {b}: a sequence holds up to {self.s_max}")
+        need = sum(m for m in more.values() if m > 0)
+        if need > len(self._free):
+            raise ValueError(f"{need} more pages needed, {len(self._free)} free")
+        for b, m in more.items():
+            if m > 0:
+                new = [self._free.pop() for _ in range(m)]
+                at = len(self._pages[b])
+                self._pages[b] += new
+                self.page_table[b, at:at + m] = torch.tensor(new, dtype=torch.int32)
+
+    def release(self, seq):
+        """Gives the sequence's pages back (its tokens are gone)."""
+        self._free += reversed(self._pages[seq])
+        self._pages[seq] = []
+        self.page_table[seq].fill_(-1)
+
+    def slots(self, pos, seq):
+        """Slots (int32) of tokens at pos of sequences seq, both int32 device tensors; -1 where a
+        sequence has no page."""
+        p = pos.long()
+        page = self.page_table[seq.long(), p // self.page_size]
+        return torch.where(page < 0, -1, page * self.page_size + (p % self.page_size).to(torch.int32))
+
+
 @dataclasses.dataclass
 class PassState:
     """Device buffers of one token pass (prefill batch or decode step)."""
@@ -60,6 +140,10 @@ class PassState:
     attn_out: torch.Tensor
     ffn_act: torch.Tensor
     workspace: torch.Tensor | None = None
+    # passes over an 8-bit cache: K and V of the pass's rows as computed, [N, n_tok, H, hd]
+    new_k: torch.Tensor | None = None
+    new_v: torch.Tensor | None = None
+    cache_slot: torch.Tensor | None = None
 
     def final_h(self, row):
         """[D] final state of a row (state at exit, or after the last layer)."""
@@ -195,6 +279,16 @@ class DecoderModel:
             v = torch.full(dims, fill, dtype=self.tdt, device=self.device)
         return KVCache(k, v, n_seq, s_max)
 
+    def new_paged_cache(self, n_seq, n_pages, page_size=64, max_pages=None, kv_dtype=None):
+        """A PagedKVCache of this model's layers; kv_dtype "fp8" or (default) the model's type;
+        max_pages: of one sequence (default: all)."""
+        s = self.shape
+        kv_dtype = self.dtype if kv_dtype is None else kv_dtype
+        if kv_dtype not in (self.dtype, "fp8"):
+            raise ValueError(f"a {self.dtype} model has a {self.dtype} or fp8 cache, not {kv_dtype}")
+        return PagedKVCache(s.n_layers, s.n_heads, s.head_dim, n_seq, n_pages, page_size,
+                            n_pages if max_pages is None else max_pages, kv_dtype, self.device)
+
     def new_state(self, n_tok, pos, seq, slot, force_layer=None):
         s, dev, tdt = self.shape, self.device, self.tdt
         i32 = dict(dtype=torch.int32, device=dev)
@@ -241,10 +335,24 @@ class DecoderModel:
         a.exited, a.exit_layer, a.exit_flag = B.ptr(st.exited), B.ptr(st.exit_layer), B.ptr(st.exit_flag)
         a.sim_out = B.ptr(st.sim_out)
         a.force_layer = B.ptr(st.force_layer)
-        a.k_cache, a.v_cache, a.n_slots = B.ptr(cache.k), B.ptr(cache.v), cache.n_slots
+        paged = isinstance(cache, PagedKVCache)
+        if paged and cache.kv_dtype == "fp8":
+            if not a.kv_fused:      # generated after each layer, where the next one finds them
+                a.attn_tiles = 1
+            if st.new_k is None:
+                dims = (s.n_layers, st.n_tok, s.n_heads, s.head_dim)
+                st.new_k = torch.empty(dims, dtype=self.tdt, device=self.device)
+                st.new_v = torch.empty(dims, dtype=self.tdt, device=self.device)
+                st.cache_slot = st.slot
+                st.slot = torch.arange(st.n_tok, dtype=torch.int32, device=self.device)
+                a.slot = B.ptr(st.slot)
+            a.k_cache, a.v_cache, a.n_slots = B.ptr(st.new_k), B.ptr(st.new_v), st.n_tok
+        else:
+            a.k_cache, a.v_cache, a.n_slots = B.ptr(cache.k), B.ptr(cache.v), cache.n_slots
         a.q_buf, a.attn_out, a.ffn_act = B.ptr(st.q_buf), B.ptr(st.attn_out), B.ptr(st.ffn_act)
         a.hsm = ctypes.addressof(self._hsm_struct) if self._hsm_struct is not None else None
-        need = B.layer_workspace_bytes(a)
+        need = (B.layer_paged_workspace_bytes(a, cache.kv, cache.max_pages) if paged
+                else B.layer_workspace_bytes(a))
         if st.workspace is None or st.workspace.numel() < need:
             st.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
         a.workspace, a.workspace_bytes = B.ptr(st.workspace), st.workspace.numel()
@@ -260,10 +368,12 @@ class DecoderModel:
 
     def token_pass(self, ids, pos, seq, cache, cfg, force_layer=None, attn_tiles=True,
                    logit_rows=None, on_layer=None):
-        """Run token rows (ids/pos/seq: int32 device tensors [n]) through all layers."""
+        """Run token rows (ids/pos/seq: int32 device tensors [n]) through all layers.  Over a
+        paged cache the rows' pages have to be reserved."""
         s = self.shape
         n = int(ids.shape[0])
-        slot = (seq * cache.s_max + pos).to(torch.int32)
+        paged = isinstance(cache, PagedKVCache)
+        slot = cache.slots(pos, seq) if paged else (seq * cache.s_max + pos).to(torch.int32)
         st = self.new_state(n, pos, seq, slot, force_layer)
         if self.gpt2:
             B.embed_positions(n, s.d_model, s.vocab, s.max_pos, ids, pos, self.embed,
@@ -273,7 +383,10 @@ class DecoderModel:
         B.token_init(n, s.n_layers, s.d_model, st.active[0], st.counts, st.exit_layer, st.inertia)
         args = self.layer_args(st, cache, cfg, attn_tiles)
         for i in range(1, s.n_layers + 1):
-            B.layer_step(args, i)
+            if paged:
+                B.layer_step_paged(args, cache.kv, cache.page_table, i, st.cache_slot)
+            else:
+                B.layer_step(args, i)
             if on_layer is not None:
                 on_layer(i, st)
         if logit_rows is None:
@@ -293,17 +406,27 @@ class DecoderModel:
         return PassResult(logits, rows, st.exit_layer, st)
 
     def prefill(self, ids, cfg, s_max=None, force_layer=None, logits="all", cache=None,
-                on_layer=None):
-        """ids: [B, T] (numpy or tensor).  logits: "all", "last" or None."""
+                on_layer=None, start=0):
+        """ids: [B, T] (numpy or tensor).  logits: "all", "last" or None.  start: position of
+        the first token, after the `start` tokens of each sequence that the (given) cache holds:
+        a prompt can be run in pieces."""
         ids = torch.as_tensor(np.asarray(ids) if not isinstance(ids, torch.Tensor) else ids)
         Bn, T = ids.shape
         s_max = T if s_max is None else s_max
         dev = self.device
+        if start < 0 or (start > 0 and cache is None):
+            raise ValueError(f"a prompt from position {start} on continues a cache")
         if cache is None:
             cache = self.new_cache(Bn, s_max)
-        pos = torch.arange(T, dtype=torch.int32, device=dev).repeat(Bn)
+        elif start or isinstance(cache, PagedKVCache):
+            s_max = cache.s_max
+        pos = torch.arange(start, start + T, dtype=torch.int32, device=dev).repeat(Bn)
         seq = torch.arange(Bn, dtype=torch.int32, device=dev).repeat_interleave(T)
-        self._check_positions(pos, s_max, pos_max=T - 1)
+        self._check_positions(pos, s_max, pos_max=start + T - 1)
+        if isinstance(cache, PagedKVCache):
+            if Bn > cache.n_seq:
+                raise ValueError(f"{Bn} sequences, the cache has {cache.n_seq}")
+            cache.reserve({b: start + T for b in range(Bn)})
         fl = None
         if isinstance(force_layer, torch.Tensor):
             fl = force_layer.reshape(-1).to(dev, torch.int32)
@@ -320,11 +443,17 @@ class DecoderModel:
 
     def decode_step(self, cache, ids, pos, cfg, force_layer=None, on_layer=None, pos_max=None):
         """One new token per sequence: ids, pos int32 device tensors [n_seq];
-        pos_max: the largest position, when known on the host (no read-back)."""
+        pos_max: the largest position, when known on the host (no read-back;
+        over a paged cache every sequence then gets the pages for it)."""
         dev = self.device
         n = int(ids.shape[0])
         seq = torch.arange(n, dtype=torch.int32, device=dev)
         self._check_positions(pos, cache.s_max, pos_max)
+        if isinstance(cache, PagedKVCache):
+            if n > cache.n_seq:
+                raise ValueError(f"{n} sequences, the cache has {cache.n_seq}")
+            at = [pos_max] * n if pos_max is not None else pos.tolist()
+            cache.reserve({b: int(p) + 1 for b, p in enumerate(at)})
         rows = torch.arange(n, dtype=torch.int32, device=dev)
         return self.token_pass(ids.to(torch.int32), pos.to(torch.int32), seq, cache, cfg,
                                force_layer, False, rows, on_layer)
