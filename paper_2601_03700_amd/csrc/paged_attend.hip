@@ -235,6 +235,32 @@ __device__ __forceinline__ bool finite(float x) {
   return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
 }
 
+// Direct loads: 16 bytes of each lane to LDS, lane l's at dst + 16 l (dst: a uniform
+// LDS address), from an address of each lane or from a uniform one and a byte
+// offset of each lane.  Waited for by wait_loads(): the compiler, where it knows of
+// such a load, puts a wait for all of them in front of every transposing LDS read.
+__device__ __forceinline__ void load_lds16(const char* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst)
+               : "memory");
+}
+__device__ __forceinline__ void load_lds16(const char* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off),
+               "s"(base), "s"(dst)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(
+      __attribute__((address_space(3))) const char*)p);
+}
+// The lane number, in a way that keeps what is formed from it where it is used
+// (not in registers across a loop that has none to spare).
+__device__ __forceinline__ int lane_here() {
+  int l = threadIdx.x & 63;
+  asm volatile("" : "+v"(l));
+  return l;
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // Column j of a tile: its entry and query head.
 __device__ __forceinline__ void column_of(const Tile& t, int j, int G, int hk, int* k, int* h) {
   const int c = t.col + j;
@@ -375,41 +401,65 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
     auto page_of = [&](int kb) { return pages[min(key_of(kb), te - 1) >> c.shift]; };
     auto slots_of = [&](int kb, int page) { return c.slot(page, key_of(kb), key_of(kb) < te); };
     const int64_t rowc = (int64_t)c.n_kv_heads * HD;    // elements of a slot
+    // Where a load's rows lie in one page and are all there, its address is a
+    // uniform base and fixed offsets of the lanes (else some 100 instructions a
+    // block, as many as the softmax takes).
+    constexpr int RUN = 64 / (FP8 ? PCH : NCH);         // rows of a wave's load
+    const bool runs = (1 << c.shift) >= RUN;
+    const uint32_t rowb = (uint32_t)(rowc * (FP8 ? 1 : 2));
+    auto base_of = [&](int op, int s) {
+      return (const char*)(op ? c.v : c.k) + s * (int64_t)rowb + hk * HD * (FP8 ? 1 : 2);
+    };
     // bf16: direct loads
-    auto issue = [&](int u, int sl) {
+    uint32_t koff[DPW], voff = 0;
+    if constexpr (!FP8) {
+#pragma unroll
+      for (int jj = 0; jj < DPW; ++jj)
+        koff[jj] = (lane / NCH) * rowb +
+                   ((lane % NCH) ^ fk((wave * DPW + jj) * RPI + lane / NCH)) * 16;
+      voff = (lane / NCH) * rowb + ((lane % NCH) ^ fv(lane / NCH)) * 16;   // fv repeats every RPI rows
+    }
+    const uint32_t lds0 = lds_address(sKV);
+    auto issue = [&](int u, int sl, bool all) {
 #pragma unroll
       for (int jj = 0; jj < DPW; ++jj) {
         const int qd = wave * DPW + jj;
-        const int r = qd * RPI + lane / NCH;
-        const int s = __shfl(sl, r, 64);
-        const int64_t at = s * rowc + hk * HD;
+        const uint32_t dst = lds0 + u * (2 * BLK) + qd * 1024;
+        if (all) {
+          const int s = __builtin_amdgcn_readlane(sl, qd * RPI);
+          load_lds16(base_of(0, s), koff[jj], dst);
+          load_lds16(base_of(1, s), voff, dst + BLK);
+        } else {
+          const int l = lane_here(), r = qd * RPI + l / NCH;
+          const int s = __shfl(sl, r, 64);
 #pragma unroll
-        for (int op = 0; op < 2; ++op) {
-          const int ch = (lane % NCH) ^ (op ? fv(r) : fk(r));
-          const char* src = (const char*)((const bf16*)(op ? c.v : c.k) + at) + ch * 16;
-          if (s < 0) src = (const char*)kZeroRow + ch * 16;
-          __builtin_amdgcn_global_load_lds(
-              (__attribute__((address_space(1))) void*)src,
-              (__attribute__((address_space(3))) void*)(&sKV[u][op][qd * 1024]), 16, 0, 0);
+          for (int op = 0; op < 2; ++op)
+            load_lds16((s < 0 ? (const char*)kZeroRow : base_of(op, s)) +
+                           ((l % NCH) ^ (op ? fv(r) : fk(r))) * 16,
+                       dst + op * BLK);
         }
       }
     };
     // 8-bit: codes and scales to registers, then as bf16 to LDS
-    uint4 code[2][PPT];
-    float csc[2][PPT];
-    auto fetch = [&](int sl) {
+    u32x4_t code[2][PPT];
+    uint8_t csc[2][PPT];
+    auto fetch = [&](int sl, bool all) {
 #pragma unroll
       for (int i = 0; i < PPT; ++i) {
-        const int pc = i * kTileThreads + tid, r = pc / PCH;
-        const int s = __shfl(sl, r, 64);
+        const int l = lane_here(), r = i * (kTileThreads / PCH) + wave * RUN + l / PCH;
+        const int s = all ? __builtin_amdgcn_readlane(sl, i * (kTileThreads / PCH) + wave * RUN)
+                          : max(__shfl(sl, r, 64), 0);
 #pragma unroll
         for (int op = 0; op < 2; ++op) {
-          code[op][i] = make_uint4(0, 0, 0, 0);
-          csc[op][i] = 1.0f;
-          if (s >= 0) {
-            const uint8_t* src = (const uint8_t*)(op ? c.v : c.k) + s * rowc + hk * HD;
-            code[op][i] = *reinterpret_cast<const uint4*>(src + pc % PCH * 16);
-            csc[op][i] = scale_of((op ? c.v_scale : c.k_scale)[(int64_t)s * c.n_kv_heads + hk]);
+          const uint8_t* sc = op ? c.v_scale : c.k_scale;
+          if (all) {
+            code[op][i] = *reinterpret_cast<const u32x4_t*>(
+                base_of(op, s) + ((l / PCH) * rowb + l % PCH * 16));
+            csc[op][i] = (sc + (int64_t)s * c.n_kv_heads + hk)[(l / PCH) * (uint32_t)c.n_kv_heads];
+          } else {
+            code[op][i] = *reinterpret_cast<const u32x4_t*>(base_of(op, s) + l % PCH * 16);
+            csc[op][i] = sc[(int64_t)s * c.n_kv_heads + hk];
+            if (__shfl(sl, r, 64) < 0) code[op][i] = u32x4_t{0, 0, 0, 0};
           }
         }
       }
@@ -420,15 +470,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
         const int pc = i * kTileThreads + tid, r = pc / PCH;
 #pragma unroll
         for (int op = 0; op < 2; ++op) {
-          const uint32_t w[4] = {code[op][i].x, code[op][i].y, code[op][i].z, code[op][i].w};
+          const float sc = scale_of(csc[op][i]);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const uint4 x = make_uint4(fp8x2_to_bf16x2<false>(w[2 * half], csc[op][i]),
-                                       fp8x2_to_bf16x2<true>(w[2 * half], csc[op][i]),
-                                       fp8x2_to_bf16x2<false>(w[2 * half + 1], csc[op][i]),
-                                       fp8x2_to_bf16x2<true>(w[2 * half + 1], csc[op][i]));
+            const uint32_t a = code[op][i][2 * half], b = code[op][i][2 * half + 1];
             const int ch = (pc % PCH * 2 + half) ^ (op ? fv(r) : fk(r));
-            *reinterpret_cast<uint4*>(&sKV[u][op][r * ROWB + ch * 16]) = x;
+            *reinterpret_cast<u32x4_t*>(&sKV[u][op][r * ROWB + ch * 16]) =
+                u32x4_t{fp8x2_to_bf16x2<false>(a, sc), fp8x2_to_bf16x2<true>(a, sc),
+                        fp8x2_to_bf16x2<false>(b, sc), fp8x2_to_bf16x2<true>(b, sc)};
           }
         }
       }
@@ -441,10 +490,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
       there = __ballot(sl >= 0);
       page = page_of(1);
       if constexpr (FP8) {
-        fetch(sl);
+        fetch(sl, false);
         put(0);
       } else {
-        issue(0, sl);
+        issue(0, sl, false);
+        wait_loads();
       }
     }
     __syncthreads();
@@ -456,7 +506,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
         const int sl = slots_of(kb + 1, page);
         there = __ballot(sl >= 0);
         page = page_of(kb + 2);
-        if constexpr (FP8) fetch(sl); else issue(u ^ 1, sl);
+        if (runs && there == ~0ull) {
+          if constexpr (FP8) fetch(sl, true); else issue(u ^ 1, sl, true);
+        } else {
+          if constexpr (FP8) fetch(sl, false); else issue(u ^ 1, sl, false);
+        }
       }
       if (t0 < wend) {
         const char* cK = sKV[u][0];
@@ -466,16 +520,25 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
         f32x16_t s[2];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
+          const int r = kt * 32 + c32;
+          bf16x8_t a[DS];
+#pragma unroll
+          for (int ds = 0; ds < DS; ++ds)
+            a[ds] = *reinterpret_cast<const bf16x8_t*>(cK + r * ROWB + ((2 * ds + hh) ^ fk(r)) * 16);
 #pragma unroll
           for (int v = 0; v < 16; ++v) s[kt][v] = 0.0f;
-          const int r = kt * 32 + c32;
 #pragma unroll
-          for (int ds = 0; ds < DS; ++ds) {
-            const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(
-                cK + r * ROWB + ((2 * ds + hh) ^ fk(r)) * 16);
-            s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[ds], s[kt], 0, 0, 0);
-          }
+          for (int ds = 0; ds < DS; ++ds)
+            s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ds], qf[ds], s[kt], 0, 0, 0);
         }
+        // a few fragments ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int x = 0; x < 2 * DS - 4; ++x) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
         __builtin_amdgcn_s_setprio(0);
         // keys that are not there, or past a column's end
         if (t0 + KB > wfull || mask != ~0ull) {
@@ -527,28 +590,39 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
         }
         // O^T += V^T P^T: in each 16-lane group source lane L reads 4 dims of
         // key k0 + L/4 and lane i receives dim n0 + i of keys k0 .. k0 + 3
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
+        // (the fragments of a dim block are read while the one before is multiplied)
+        const int r0 = 4 * hh + ((lane & 15) >> 2);
+        auto read_v = [&](int db, bf16x8_t (&a)[4]) {
+          const int ch = db * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+          const char* at = cV + r0 * ROWB + ((ch ^ fv(r0)) * 16) + 8 * (lane & 1);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             s16x4 half[2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int r = 16 * i + 8 * x + 4 * hh + ((lane & 15) >> 2);
-              const int ch = db * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            for (int x = 0; x < 2; ++x)     // fv repeats every 4 rows
               half[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (lds_s16x4*)(cV + r * ROWB + ((ch ^ fv(r)) * 16) + 8 * (lane & 1)));
-            }
-            const bf16x8_t a = __builtin_bit_cast(
+                  (lds_s16x4*)(at + (16 * i + 8 * x) * ROWB));
+            a[i] = __builtin_bit_cast(
                 bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
-            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[i], o[db], 0, 0, 0);
           }
+        };
+        bf16x8_t va[2][4];
+        read_v(0, va[0]);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          if (db + 1 < DB) read_v(db + 1, va[(db + 1) & 1]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[db & 1][i], pb[i], o[db], 0, 0, 0);
+        }
         __builtin_amdgcn_s_setprio(0);
       }
       if constexpr (FP8) {
         if (kb + 1 < nkb) put(u ^ 1);
       }
+      if constexpr (!FP8) wait_loads();
       __syncthreads();   // block kb + 1 landed, stage u is free
     }
 
