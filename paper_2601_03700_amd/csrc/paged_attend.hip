@@ -208,7 +208,9 @@ constexpr int kTileThreads = 256;
 __device__ const uint4 kZeroRow[16] = {};
 
 // max(a, b, c) without quieting the matrix products' results first (fmaxf
-// would: one more instruction a value)
+// would: one more instruction a value).  The compiler does not see that this
+// reads a product's result and puts no wait for it: the first maximum over a
+// product's result is taken by fmaxf, the others depend on it.
 __device__ __forceinline__ float max3_raw(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
@@ -553,13 +555,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
         }
         // the block's maximum of the column; the reference maximum moves (and o
         // is rescaled) only where a block exceeds it by more than 2^kLazy
-        float mb = max3_raw(s[0][0], s[0][1], s[0][2]);
+        float mb = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
-        for (int v = 3; v < 15; v += 2) mb = max3_raw(mb, s[0][v], s[0][v + 1]);
-        mb = max3_raw(mb, s[0][15], s[1][0]);
-#pragma unroll
-        for (int v = 1; v < 15; v += 2) mb = max3_raw(mb, s[1][v], s[1][v + 1]);
-        mb = max_halves(max3_raw(mb, s[1][15], mb)) * scale_log2;
+        for (int v = 1; v < 16; ++v) mb = max3_raw(mb, s[0][v], s[1][v]);
+        mb = max_halves(mb) * scale_log2;
         if (__any(mb > m_ref + kLazy)) {
           const float mn = fmaxf(m_ref, mb);
           const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_ref - mn);
@@ -1191,10 +1190,10 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
         for (int v = 0; v < 4; ++v)
           s[sb][v] = (mask >> (sb * 16 + 4 * g + v)) & 1 ? s[sb][v] : -INFINITY;
     }
-    float mb = max3_raw(s[0][0], s[0][1], s[0][2]);
-    mb = max3_raw(mb, s[0][3], s[1][0]);
-    mb = max3_raw(mb, s[1][1], s[1][2]);
-    mb = max_column(max3_raw(mb, s[1][3], mb)) * scale_log2;
+    float mb = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+    for (int v = 1; v < 4; ++v) mb = max3_raw(mb, s[0][v], s[1][v]);
+    mb = max_column(mb) * scale_log2;
     if (__any(mb > m_ref + kLazy)) {
       const float mn = fmaxf(m_ref, mb);
       const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_ref - mn);

@@ -302,6 +302,20 @@ def test_same_bits_each_time_and_in_a_graph(dt, cache, chunk):
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("shape", [[(900, 33, 1), (70, 33, 1)], [(300, 33, 1)],
+                                   [(900, 1, 1), (70, 1, 1), (5, 1, 1)]])
+def test_the_same_bits_ten_times(cache, hd, shape):
+    """Nothing left over in registers or LDS enters a result, the choice of the softmax's
+    reference among it."""
+    print(f"paged attend, ten times, bf16/{cache} hd={hd} {shape}", flush=True)
+    c = Case("bf16", cache, 8, 2, hd, 16, shape, seed=2)
+    first = c.check()
+    for _ in range(10):
+        assert torch.equal(c.run(), first)
+
+
 def test_chunks_are_written_and_attended_in_turn():
     """A prompt in pieces of different lengths through the 8-bit and the bf16 cache, then single
     tokens, as a program runs it: each step's rows are stored, then attended with, and the cache
