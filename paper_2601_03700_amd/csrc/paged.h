@@ -44,14 +44,16 @@ struct Entries {
   const int32_t *rows, *n_active, *pos, *seq, *key_len;
   int max_active, causal;
 };
-__device__ __forceinline__ int entry_limit(const Entries& e, const PagedView& c, int row, int* seq) {
-  const int b = e.seq[row];
-  *seq = b;
-  if ((unsigned)b >= (unsigned)c.n_seq) return 0;
+__device__ __forceinline__ int key_limit(const Entries& e, const PagedView& c, int seq, int pos) {
+  if ((unsigned)seq >= (unsigned)c.n_seq) return 0;
   int n = c.max_pages << c.shift;
-  if (e.causal) n = min(n, min(e.pos[row], INT_MAX - 1) + 1);
-  if (e.key_len) n = min(n, e.key_len[b]);
+  if (e.causal) n = min(n, min(pos, INT_MAX - 1) + 1);
+  if (e.key_len) n = min(n, e.key_len[seq]);
   return max(n, 0);
+}
+__device__ __forceinline__ int entry_limit(const Entries& e, const PagedView& c, int row, int* seq) {
+  *seq = e.seq[row];
+  return key_limit(e, c, *seq, e.causal ? e.pos[row] : 0);
 }
 
 constexpr int kMaxEntries = 1 << 23;   // rows or entries of a call (its grid's bound)

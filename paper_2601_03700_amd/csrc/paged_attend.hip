@@ -109,21 +109,22 @@ constexpr int TC_ = 128;       // columns of a tile
 constexpr int kPlanThreads = 1024;
 
 // Columns of one sequence's entries (a stretch of the list from entry `first`
-// on, G columns each): columns col .. col + cols - 1, cols <= TC_.
+// on, G columns each): columns col .. col + cols - 1, cols <= TC_ (0: no tile).
 struct Tile {
   int first, col, cols, seq;
 };
 
 // Segments: stretches of entries of one sequence.  Each pass takes 8 entries of
-// every thread, all loads of the pass in flight together, and ranks the starts
-// by wave ballots; then a scan over the segments' tile counts.  starts:
-// [max_active + 1].
-__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Entries e, int G,
-                                                                  int32_t* __restrict__ starts,
-                                                                  Tile* __restrict__ tiles,
-                                                                  int32_t* __restrict__ n_tiles) {
+// every thread, all loads of the pass in flight together, and ranks the starts by
+// wave ballots; then a scan over the segments' tile counts.  starts:
+// [max_active + 1].  One workgroup, whose chain of loads is what it takes: 4 us for
+// 500 entries, 14 for 16384.  (The entries' limits and the tiles' ends formed here
+// too, to shorten the start of the tiles' workgroups: 8 and 29 us, and no more won.)
+__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(
+    Entries e, int G, int max_tiles, int32_t* __restrict__ starts, Tile* __restrict__ tiles,
+    int32_t* __restrict__ n_tiles) {
   constexpr int U = 8, W = kPlanThreads / 64;
-  __shared__ int cnt[U * W], base_s;
+  __shared__ int cnt[U * W], base_s, nt_s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = min(*e.n_active, e.max_active);
   if (tid == 0) base_s = 0;
@@ -143,21 +144,28 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Entries e, int
     uint64_t m[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      m[u] = __ballot(k0 + u * kPlanThreads + tid < n && at[u] != before[u]);
+      const int k = k0 + u * kPlanThreads + tid;
+      m[u] = __ballot(k < n && at[u] != before[u]);
       if (lane == 0) cnt[u * W + wave] = __popcll(m[u]);
     }
     __syncthreads();
-    if (wave == 0) {               // exclusive ranks of the U * W = 128 counts
-      const int a = cnt[2 * lane], b = cnt[2 * lane + 1];
-      int x = a + b;
+    if (wave == 0) {               // exclusive ranks of the U * W counts
+      constexpr int P = U * W / 64;
+      int c4[P], sum = 0;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        c4[i] = sum;
+        sum += cnt[P * lane + i];
+      }
+      int x = sum;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const int y = __shfl_up(x, o, 64);
         if (lane >= o) x += y;
       }
-      const int base = base_s + x - a - b;
-      cnt[2 * lane] = base;
-      cnt[2 * lane + 1] = base + a;
+      const int base = base_s + x - sum;
+#pragma unroll
+      for (int i = 0; i < P; ++i) cnt[P * lane + i] = base + c4[i];
       if (lane == 63) base_s += x;
     }
     __syncthreads();
@@ -171,26 +179,43 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Entries e, int
   const int ns = n > 0 ? base_s : 0;
   if (tid == 0) starts[ns] = n;
   __syncthreads();                 // starts are this workgroup's own writes
-  if (wave != 0) return;
-  int acc = 0;
-  for (int i0 = 0; i0 < ns; i0 += 64) {
-    const int i = i0 + lane;
-    const int first = i < ns ? starts[i] : 0;
-    const int64_t cols = i < ns ? (int64_t)(starts[i + 1] - first) * G : 0;
-    const int nt = (int)((cols + TC_ - 1) / TC_);
-    int x = nt;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(x, o, 64);
-      if (lane >= o) x += y;
+  if (wave == 0) {                 // the segments' tiles, 64 segments at a time
+    int acc = 0;
+    for (int i0 = 0; i0 < ns; i0 += 64) {
+      const int i = i0 + lane;
+      const int first = i < ns ? starts[i] : 0, next = i < ns ? starts[i + 1] : 0;
+      const int64_t cols = (int64_t)(next - first) * G;
+      const int mine = (int)((cols + TC_ - 1) / TC_);
+      const int seq = i < ns ? e.seq[e.rows[first]] : 0;
+      // all first tiles, all second ones, ...: those of the same place in their
+      // prompts next to each other
+      for (int t = 0;; ++t) {
+        const uint64_t more = __ballot(mine > t);
+        if (more == 0) break;
+        if ((more & (more - 1)) == 0) {      // one segment's rest: a lane a tile
+          const int j = __ffsll((unsigned long long)more) - 1;
+          const int f = __builtin_amdgcn_readlane(first, j), b = __builtin_amdgcn_readlane(seq, j);
+          const int nj = __builtin_amdgcn_readlane(mine, j);
+          const int64_t cj = (int64_t)(__builtin_amdgcn_readlane(next, j) - f) * G;
+          for (int u = t + lane; u < nj; u += 64)
+            tiles[acc + u - t] = Tile{f, u * TC_, (int)min((int64_t)TC_, cj - (int64_t)u * TC_), b};
+          acc += nj - t;
+          break;
+        }
+        if (mine > t)
+          tiles[acc + __popcll(more & ((1ull << lane) - 1))] =
+              Tile{first, t * TC_, (int)min((int64_t)TC_, cols - (int64_t)t * TC_), seq};
+        acc += __popcll(more);
+      }
     }
-    const int seq = i < ns ? e.seq[e.rows[first]] : 0;
-    for (int t = 0; t < nt; ++t)
-      tiles[acc + x - nt + t] =
-          Tile{first, t * TC_, (int)min((int64_t)TC_, cols - (int64_t)t * TC_), seq};
-    acc += __shfl(x, 63, 64);
+    if (lane == 0) {
+      *n_tiles = acc;
+      nt_s = acc;
+    }
   }
-  if (lane == 0) *n_tiles = acc;
+  __syncthreads();
+  const int nt = nt_s;
+  for (int t = nt + tid; t < max_tiles; t += kPlanThreads) tiles[t] = Tile{0, 0, 0, 0};
 }
 
 // ---------------------------------------------------------------------------
@@ -270,8 +295,8 @@ __device__ __forceinline__ void column_of(const Tile& t, int j, int G, int hk, i
   *h = hk * G + c % G;
 }
 
-// Work item of a workgroup, head by head: position in the order of the tiles
-// (-1: none), K/V head, part of the keys.  The hardware deals workgroups
+// Work item of a workgroup, head by head: tile (-1: none), K/V head, part of the
+// keys.  The hardware deals workgroups
 // round-robin to the 8 XCDs: with 8 K/V heads or more each XCD takes a run of
 // items, so that the tiles in flight on it share a few heads' K/V in its L2;
 // with fewer heads the items are dealt as they come, which keeps the XCDs evenly
@@ -287,25 +312,39 @@ __device__ __forceinline__ TileItem tile_item(int max_tiles, int heads, int part
     const int per = (total + 7) >> 3;
     item = (int)(blockIdx.x >> 3) < per ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : total;
   }
-  TileItem t{item / parts % max_tiles, item / parts / max_tiles, item % parts, parts == 1};
+  // the last tiles first: of prompts, the longest
+  TileItem t{max_tiles - 1 - item / parts % max_tiles, item / parts / max_tiles, item % parts,
+             parts == 1};
   // a list whose sequences are scattered can hold more tiles than the host
   // counted on: then each workgroup takes several, with all of their keys
   if (nt > max_tiles) t.whole = true;
-  if (item >= total || t.tile >= nt || (t.whole && t.part > 0)) t.tile = -1;
+  if (item >= total || (t.whole && t.part > 0)) t.tile = -1;
   return t;
 }
-// The keys that some column of the tile sees: 0 .. result - 1.
-__device__ __forceinline__ int tile_end(const Entries& e, const PagedView& c, const Tile& tile, int G,
-                                        int hk) {
-  int n = 0;
-  for (int j = threadIdx.x & 63; j < tile.cols; j += 64) {
-    int k, h, b;
-    column_of(tile, j, G, hk, &k, &h);
-    n = max(n, entry_limit(e, c, e.rows[k], &b));
+// The limits of the tile's columns: *n: keys that some column sees (0 .. *n - 1);
+// returns column j's.  Every wave reads all columns' (two a lane).
+__device__ __forceinline__ int tile_limits(const Entries& e, const PagedView& c, const Tile& tile,
+                                           int G, int hk, int j, int* n) {
+  static_assert(TC_ == 128, "two columns a lane");
+  const int lane = threadIdx.x & 63;
+  int row[2], lim[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int k, h;
+    column_of(tile, min(lane + 64 * i, tile.cols - 1), G, hk, &k, &h);
+    row[i] = e.rows[k];
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) n = max(n, __shfl_xor(n, o, 64));
-  return __builtin_amdgcn_readfirstlane(n);
+  for (int i = 0; i < 2; ++i) {
+    int b;
+    lim[i] = entry_limit(e, c, row[i], &b);     // columns past the last repeat it
+  }
+  int m = max(lim[0], lim[1]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o, 64));
+  *n = __builtin_amdgcn_readfirstlane(m);
+  const int a = __shfl(lim[0], j & 63, 64), b = __shfl(lim[1], j & 63, 64);
+  return j >= tile.cols ? 0 : j < 64 ? a : b;
 }
 __device__ __forceinline__ void part_keys(int n, int parts, int p, int* t0, int* t1) {
   const int per = ((n + KB - 1) / KB + parts - 1) / parts * KB;
@@ -320,8 +359,15 @@ __device__ __forceinline__ void part_keys(int n, int parts, int p, int* t0, int*
 // takes one lane swap, and the weights already lie as the B operand of
 // O^T += V^T P^T wants them, if V^T is read in the same order of keys.
 //
-// K and V come in blocks of 64 keys, bf16 in LDS in two stages, block kb + 1
-// on its way while block kb is computed.  A bf16 cache is copied there by
+// K and V come in blocks of 64 keys, bf16 in LDS.  A wave works on 32 keys at a
+// time: the scores of the next 32 are formed beside the exponentials of these (a
+// matrix instruction runs 32 cycles and takes 4 to issue), then these are
+// multiplied into the output.  So K of block kb + 1 is needed before V of block kb
+// is done with: two stages of K, three of V, one barrier a block, block kb + 2 on
+// its way while block kb + 1 is computed.  Bound by the SIMDs' instruction issue:
+// a 64-key block of a wave takes some 1900 cycles of its SIMD, 1024 of them matrix
+// instructions, the exponentials 512 and the rest of the softmax about 450.  8
+// prompts of 2048 tokens, 32 heads of 128: 360 us (0.75 PFLOP/s).  A bf16 cache is copied there by
 // direct loads; an 8-bit one goes through registers, where its codes become
 // bf16 with their scale in the conversion itself (exactly).  The slot of key
 // t0 + lane is found by every wave (its page read a block earlier: the wait for
@@ -336,8 +382,9 @@ __device__ __forceinline__ void part_keys(int n, int parts, int p, int* t0, int*
 template <int HD, bool FP8>
 __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
     int H, float scale_log2, const bf16* __restrict__ q, Entries e, PagedView c,
-    const Tile* __restrict__ tiles, const int32_t* __restrict__ n_tiles, int max_tiles, int parts,
-    bf16* __restrict__ out, float* __restrict__ part) {
+    const Tile* __restrict__ tiles, const int32_t* __restrict__ n_tiles,
+    int max_tiles, int parts, bf16* __restrict__ out,
+    float* __restrict__ part) {
   constexpr int DS = HD / 16;               // 16-dim steps of S
   constexpr int DB = HD / 32;               // 32-dim blocks of O^T
   constexpr int ROWB = HD * 2;              // bytes of a row in LDS
@@ -345,9 +392,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
   constexpr int RPI = 1024 / ROWB;          // rows of one direct load of a wave
   constexpr int DPW = KB / RPI / 4;         // direct loads of a wave and operand
   constexpr int BLK = KB * ROWB;
+  constexpr int NCO = ROWB / 16;            // chunks of a row of the output
   // 8-bit cache: 16-byte pieces of a row, and how many of a block a thread takes
   constexpr int PCH = HD / 16, PPT = KB * PCH / kTileThreads;
-  __shared__ __attribute__((aligned(1024))) char sKV[2][2][BLK];
+  __shared__ __attribute__((aligned(1024))) char sK[2][BLK], sV[3][BLK];
 
   const int G = H / c.n_kv_heads;
   const int nt = *n_tiles;
@@ -362,29 +410,21 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
   auto fv = [](int r) { return HD == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
 
   for (int ti = it.tile; ti < nt; ti += max_tiles) {
-    const Tile tile = tiles[nt - 1 - ti];   // of a prompt, the latest (longest) first
+    const Tile tile = tiles[ti];
+    if (tile.cols == 0) return;
     const int32_t* pages = c.table + (int64_t)tile.seq * c.max_pages;
-    const int tend = tile_end(e, c, tile, G, hk);
     const int j = wave * 32 + c32;
     const bool valid = j < tile.cols;
-    int qk, qh, qlim = 0;
-    column_of(tile, valid ? j : 0, G, hk, &qk, &qh);
-    const int64_t qat = ((int64_t)qk * H + qh) * HD;
-    if (valid) {
-      int b;
-      qlim = entry_limit(e, c, e.rows[qk], &b);
-    }
-    int wend = qlim, wfull = valid ? qlim : INT_MAX;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      wend = max(wend, __shfl_xor(wend, o, 64));
-      wfull = min(wfull, __shfl_xor(wfull, o, 64));
-    }
-    wend = __builtin_amdgcn_readfirstlane(wend);     // the wave's columns see keys below it,
-    wfull = __builtin_amdgcn_readfirstlane(wfull);   // and all of them the ones below this
-    int tb, te;
+    int tend, tb, te;
+    const int qlim = tile_limits(e, c, tile, G, hk, j, &tend);
     part_keys(tend, whole ? 1 : parts, p, &tb, &te);
     const int nkb = (te - tb + KB - 1) / KB;
+    auto key_of = [&](int kb) { return tb + kb * KB + lane; };
+    auto page_of = [&](int kb) { return pages[min(key_of(kb), te - 1) >> c.shift]; };
+    int page = nkb > 0 ? page_of(0) : 0;
+    int qk, qh;
+    column_of(tile, valid ? j : 0, G, hk, &qk, &qh);
+    const int64_t qat = ((int64_t)qk * H + qh) * HD;
 
     bf16x8_t qf[DS];
 #pragma unroll
@@ -398,9 +438,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
       for (int v = 0; v < 16; ++v) o[i][v] = 0.0f;
     float m_ref = -INFINITY, l_run = 0.0f;
 
-    // keys of a block, one per lane; block kb + 1's pages are read during block kb - 1
-    auto key_of = [&](int kb) { return tb + kb * KB + lane; };
-    auto page_of = [&](int kb) { return pages[min(key_of(kb), te - 1) >> c.shift]; };
+    // slots of a block's keys, one per lane; block kb + 1's pages are read during block kb - 1
     auto slots_of = [&](int kb, int page) { return c.slot(page, key_of(kb), key_of(kb) < te); };
     const int64_t rowc = (int64_t)c.n_kv_heads * HD;    // elements of a slot
     // Where a load's rows lie in one page and are all there, its address is a
@@ -413,32 +451,29 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
       return (const char*)(op ? c.v : c.k) + s * (int64_t)rowb + hk * HD * (FP8 ? 1 : 2);
     };
     // bf16: direct loads
-    uint32_t koff[DPW], voff = 0;
-    if constexpr (!FP8) {
-#pragma unroll
-      for (int jj = 0; jj < DPW; ++jj)
-        koff[jj] = (lane / NCH) * rowb +
-                   ((lane % NCH) ^ fk((wave * DPW + jj) * RPI + lane / NCH)) * 16;
-      voff = (lane / NCH) * rowb + ((lane % NCH) ^ fv(lane / NCH)) * 16;   // fv repeats every RPI rows
-    }
-    const uint32_t lds0 = lds_address(sKV);
-    auto issue = [&](int u, int sl, bool all) {
+    // (lane offsets: load jj's K rows lie 4 jj chunks further in fk, fv repeats
+    // every RPI rows)
+    const uint32_t koff = (lane / NCH) * rowb + ((lane % NCH) ^ fk(lane / NCH)) * 16;
+    const uint32_t voff = (lane / NCH) * rowb + ((lane % NCH) ^ fv(lane / NCH)) * 16;
+    const uint32_t ldsK = lds_address(sK), ldsV = lds_address(sV);
+    auto issue_run = [&](int jj, uint32_t ko, uint32_t vo, int sl) {
+      const int qd = wave * DPW + jj, s = __builtin_amdgcn_readlane(sl, qd * RPI);
+      load_lds16(base_of(0, s), koff ^ (64 * jj), ldsK + ko + qd * 1024);
+      load_lds16(base_of(1, s), voff, ldsV + vo + qd * 1024);
+    };
+    auto issue = [&](uint32_t ko, uint32_t vo, int sl) {
 #pragma unroll
       for (int jj = 0; jj < DPW; ++jj) {
         const int qd = wave * DPW + jj;
-        const uint32_t dst = lds0 + u * (2 * BLK) + qd * 1024;
-        if (all) {
-          const int s = __builtin_amdgcn_readlane(sl, qd * RPI);
-          load_lds16(base_of(0, s), koff[jj], dst);
-          load_lds16(base_of(1, s), voff, dst + BLK);
-        } else {
+        const uint32_t dst[2] = {ldsK + ko + qd * 1024, ldsV + vo + qd * 1024};
+        {
           const int l = lane_here(), r = qd * RPI + l / NCH;
           const int s = __shfl(sl, r, 64);
 #pragma unroll
           for (int op = 0; op < 2; ++op)
             load_lds16((s < 0 ? (const char*)kZeroRow : base_of(op, s)) +
                            ((l % NCH) ^ (op ? fv(r) : fk(r))) * 16,
-                       dst + op * BLK);
+                       dst[op]);
         }
       }
     };
@@ -466,18 +501,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
         }
       }
     };
-    auto put = [&](int u) {
+    auto put = [&](uint32_t ko, uint32_t vo) {
 #pragma unroll
       for (int i = 0; i < PPT; ++i) {
         const int pc = i * kTileThreads + tid, r = pc / PCH;
 #pragma unroll
         for (int op = 0; op < 2; ++op) {
+          char* row = (op ? &sV[0][0] + vo : &sK[0][0] + ko) + r * ROWB;
           const float sc = scale_of(csc[op][i]);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             const uint32_t a = code[op][i][2 * half], b = code[op][i][2 * half + 1];
             const int ch = (pc % PCH * 2 + half) ^ (op ? fv(r) : fk(r));
-            *reinterpret_cast<u32x4_t*>(&sKV[u][op][r * ROWB + ch * 16]) =
+            *reinterpret_cast<u32x4_t*>(row + ch * 16) =
                 u32x4_t{fp8x2_to_bf16x2<false>(a, sc), fp8x2_to_bf16x2<true>(a, sc),
                         fp8x2_to_bf16x2<false>(b, sc), fp8x2_to_bf16x2<true>(b, sc)};
           }
@@ -485,173 +521,249 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
       }
     };
 
+    // block kb: its loads, from the slots of its keys; `there` is their mask.  Those
+    // of a bf16 block whose loads are runs are left to the step (returns true): eight
+    // in a row would hold the wave for some 800 cycles.
     uint64_t there = 0;
-    int page = 0;
-    if (nkb > 0) {
-      const int sl = slots_of(0, page_of(0));
+    int sl = -1;
+    auto load = [&](int kb, uint32_t ko, uint32_t vo) {
+      sl = slots_of(kb, page);
       there = __ballot(sl >= 0);
-      page = page_of(1);
+      page = page_of(kb + 1);
+      const bool run = runs && there == ~0ull;
       if constexpr (FP8) {
-        fetch(sl, false);
-        put(0);
+        if (run) fetch(sl, true); else fetch(sl, false);
+        return false;
       } else {
-        issue(0, sl, false);
-        wait_loads();
+        if (!run) issue(ko, vo, sl);
+        return run;
+      }
+    };
+    auto landed = [&](uint32_t ko, uint32_t vo) {
+      if constexpr (FP8) put(ko, vo); else wait_loads();
+    };
+    // LDS addresses of this lane's fragments: K step ds at ka ^ 32 ds (fk only
+    // touches the chunk bits), V^T block db at va ^ 64 db
+    typedef __attribute__((address_space(3))) const bf16x8_t lds_bf16x8;
+    const int r0 = 4 * hh + ((lane & 15) >> 2);
+    const uint32_t ka0 = ldsK + c32 * ROWB + ((hh ^ fk(c32)) * 16);
+    const uint32_t va0 = ldsV + r0 * ROWB +
+                         (fv(r0) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+    auto read_k = [&](uint32_t ka, int ds) { return *(lds_bf16x8*)(uintptr_t)(ka ^ (32 * ds)); };
+    // scores of 32 keys
+    auto scores = [&](uint32_t ka, f32x16_t& s) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = 0.0f;
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(ka, ds), qf[ds], s, 0, 0, 0);
+    };
+    auto column_max = [&](const f32x16_t& s) {
+      float m = fmaxf(s[0], s[1]);
+#pragma unroll
+      for (int v = 2; v < 16; v += 2) m = max3_raw(m, s[v], s[v + 1]);
+      return m;
+    };
+    // the reference maximum moves (and o is rescaled) only where new scores
+    // exceed it by more than 2^kLazy
+    auto raise = [&](float m) {
+      if (!__any(m * scale_log2 > m_ref + kLazy)) return;
+      const float mb = max_halves(m) * scale_log2;
+      const float mn = fmaxf(m_ref, mb);
+      const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_ref - mn);
+      m_ref = mn;
+      l_run *= alpha;
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[i][v] *= alpha;
+    };
+    // V^T fragments of dim block db and 32 keys: in each 16-lane group source lane
+    // L reads 4 dims of key k0 + L/4 and lane i receives dim n0 + i of keys k0 ..
+    // k0 + 3
+    auto read_v = [&](uint32_t va, int db, bf16x8_t (&a)[2]) {
+      const uint32_t at = va ^ (64 * db);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        s16x4 half[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)     // fv repeats every 4 rows
+          half[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_s16x4*)(uintptr_t)(at + (16 * i + 8 * x) * ROWB));
+        a[i] = __builtin_bit_cast(bf16x8_t,
+                                  __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+    };
+    // One step of the pipeline: the scores `sn` of the next 32 keys (K at ka) beside
+    // the weights of these 32 (scores sc), two exponentials to a product; then these
+    // into the output (V at va) beside the maximum of sn, which is returned.  The
+    // weights are rounded to bf16 (the sum takes the rounded ones, as the product
+    // does).  run: loads on the way, one pair to a product.
+    auto step = [&](bool run, uint32_t ka, f32x16_t& sn, uint32_t va, const f32x16_t& sc,
+                    uint32_t ko, uint32_t vo) {
+      constexpr int AHEAD = 3, EPS = 16 / DS;    // fragments read ahead, weights of a product
+      constexpr bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
+      const float msub = m_ref == -INFINITY ? 0.0f : m_ref;
+      bf16x8_t a[DS], v[2][2];
+#pragma unroll
+      for (int ds = 0; ds < AHEAD; ++ds) a[ds] = read_k(ka, ds);
+      uint32_t w[8];
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) {
+        if (ds == 0)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) sn[x] = 0.0f;
+        sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ds], qf[ds], sn, 0, 0, 0);
+        if (ds + AHEAD < DS) a[ds + AHEAD] = read_k(ka, ds + AHEAD);
+        if (ds == DS - 2) read_v(va, 0, v[0]);
+#pragma unroll
+        for (int x = ds * EPS; x < (ds + 1) * EPS; x += 2) {
+          w[x / 2] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(sc[x], scale_log2, -msub)),
+                                 __builtin_amdgcn_exp2f(fmaf(sc[x + 1], scale_log2, -msub)));
+          l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[x / 2]), ones,
+                                                  l_run, false);
+        }
+        if constexpr (!FP8)
+          if (run && ds % (DS / DPW) == DS / DPW - 1) issue_run(ds / (DS / DPW), ko, vo, sl);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      bf16x8_t pb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        pb[i] = __builtin_bit_cast(
+            bf16x8_t, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+      float m = 0.0f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        if (db + 1 < DB) read_v(va, db + 1, v[(db + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[db & 1][i], pb[i], o[db], 0, 0, 0);
+#pragma unroll
+        for (int x = db * (16 / DB); x < (db + 1) * (16 / DB); x += 2)
+          m = x == 0 ? fmaxf(sn[0], sn[1]) : max3_raw(m, sn[x], sn[x + 1]);
+      }
+      return m;
+    };
+
+    uint64_t mask = 0, mask1 = 0;      // of blocks kb and kb + 1
+    f32x16_t s[2];
+    if (nkb > 0) {
+      if (load(0, 0, 0))
+#pragma unroll
+        for (int jj = 0; jj < DPW; ++jj) issue_run(jj, 0, 0, sl);
+      mask = there;
+    }
+    int wend = qlim, wfull = valid ? qlim : INT_MAX;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      wend = max(wend, __shfl_xor(wend, o, 64));
+      wfull = min(wfull, __shfl_xor(wfull, o, 64));
+    }
+    wend = __builtin_amdgcn_readfirstlane(wend);     // the wave's columns see keys below it,
+    wfull = __builtin_amdgcn_readfirstlane(wfull);   // and all of them the ones below this
+    // waited for here: a wait inside the loop would be one for the loads on their way
+#pragma unroll
+    for (int s = 0; s < DS; ++s) asm volatile("" : "+v"(qf[s]));
+    // keys past a column's end, or that are not there; m: the maximum, then formed again
+    auto hide = [&](int t0, uint64_t mask, int kt, f32x16_t& s, float& m) {
+      if (t0 + KB <= wfull && mask == ~0ull) return;
+      const int h4 = 4 * (lane_here() >> 5);
+      const int lim = qlim - t0 - kt * 32 - h4;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = 8 * (v >> 2) + (v & 3) < lim ? s[v] : -INFINITY;
+      if (mask != ~0ull) {
+        const uint32_t mk = (uint32_t)(mask >> (kt * 32)) >> h4;
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          s[v] = mk & (1u << (8 * (v >> 2) + (v & 3))) ? s[v] : -INFINITY;
+      }
+      m = column_max(s);
+    };
+    constexpr uint32_t HALF = 32 * ROWB;
+    if (nkb > 0) {
+      landed(0, 0);
+      __syncthreads();
+      if (nkb > 1 && load(1, BLK, BLK))
+#pragma unroll
+        for (int jj = 0; jj < DPW; ++jj) issue_run(jj, BLK, BLK, sl);
+      mask1 = there;
+      if (tb < wend) {
+        scores(ka0, s[0]);
+        float m = column_max(s[0]);
+        hide(tb, mask, 0, s[0], m);
+        raise(m);
       }
     }
-    __syncthreads();
+    uint32_t vo = 0, von = BLK;        // of block kb's V and of block kb + 1's
     for (int kb = 0; kb < nkb; ++kb) {
-      const int u = kb & 1, t0 = tb + kb * KB;
-      const uint64_t mask = there;
-      // the other stage was last read in block kb - 1
-      if (kb + 1 < nkb) {
-        const int sl = slots_of(kb + 1, page);
-        there = __ballot(sl >= 0);
-        page = page_of(kb + 2);
-        if (runs && there == ~0ull) {
-          if constexpr (FP8) fetch(sl, true); else issue(u ^ 1, sl, true);
-        } else {
-          if constexpr (FP8) fetch(sl, false); else issue(u ^ 1, sl, false);
-        }
+      const int t0 = tb + kb * KB;
+      const uint32_t ko = (kb & 1) * BLK, von2 = von == 2 * BLK ? 0 : von + BLK;
+      if (t0 < wend) {     // a wave whose columns have seen their keys only loads
+        float m = step(false, ka0 + ko + HALF, s[1], va0 + vo, s[0], 0, 0);
+        hide(t0, mask, 1, s[1], m);
+        raise(m);
       }
-      if (t0 < wend) {
-        const char* cK = sKV[u][0];
-        const char* cV = sKV[u][1];
-        // S^T = K Q^T
-        __builtin_amdgcn_s_setprio(1);
-        f32x16_t s[2];
+      if (kb + 1 < nkb) landed(ko ^ BLK, von);
+      __syncthreads();     // block kb + 1 is in LDS; K of kb and V of kb - 1 are free
+      const bool run = kb + 2 < nkb && load(kb + 2, ko, von2);
+      if (t0 + 32 < wend) {
+        // (behind the last block: scores that are not used)
+        const uint32_t ka = ka0 + (ko ^ BLK), va = va0 + vo + HALF;
+        float m = step(run, ka, s[0], va, s[1], ko, von2);
+        hide(t0 + KB, mask1, 0, s[0], m);
+        if (kb + 1 < nkb) raise(m);
+      } else if (run) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          const int r = kt * 32 + c32;
-          bf16x8_t a[DS];
-#pragma unroll
-          for (int ds = 0; ds < DS; ++ds)
-            a[ds] = *reinterpret_cast<const bf16x8_t*>(cK + r * ROWB + ((2 * ds + hh) ^ fk(r)) * 16);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) s[kt][v] = 0.0f;
-#pragma unroll
-          for (int ds = 0; ds < DS; ++ds)
-            s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ds], qf[ds], s[kt], 0, 0, 0);
-        }
-        // a few fragments ahead of the products
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-        for (int x = 0; x < 2 * DS - 4; ++x) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-        __builtin_amdgcn_s_setprio(0);
-        // keys that are not there, or past a column's end
-        if (t0 + KB > wfull || mask != ~0ull) {
-#pragma unroll
-          for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              const int kl = kt * 32 + 8 * (v >> 2) + 4 * hh + (v & 3);
-              const bool keep = t0 + kl < qlim && ((mask >> kl) & 1);
-              s[kt][v] = keep ? s[kt][v] : -INFINITY;
-            }
-        }
-        // the block's maximum of the column; the reference maximum moves (and o
-        // is rescaled) only where a block exceeds it by more than 2^kLazy
-        float mb = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-        for (int v = 1; v < 16; ++v) mb = max3_raw(mb, s[0][v], s[1][v]);
-        mb = max_halves(mb) * scale_log2;
-        if (__any(mb > m_ref + kLazy)) {
-          const float mn = fmaxf(m_ref, mb);
-          const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_ref - mn);
-          m_ref = mn;
-          l_run *= alpha;
-#pragma unroll
-          for (int i = 0; i < DB; ++i)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) o[i][v] *= alpha;
-        }
-        // weights, rounded to bf16 (the sum takes the rounded ones, as the
-        // product does), as the B operand: 16 keys a step
-        bf16x8_t pb[4];
-        const float msub = m_ref == -INFINITY ? 0.0f : m_ref;
-        constexpr bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t w[4];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const float a = s[i >> 1][8 * (i & 1) + 2 * x], b = s[i >> 1][8 * (i & 1) + 2 * x + 1];
-            w[x] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(a, scale_log2, -msub)),
-                               __builtin_amdgcn_exp2f(fmaf(b, scale_log2, -msub)));
-            l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[x]), ones,
-                                                    l_run, false);
-          }
-          pb[i] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-        // O^T += V^T P^T: in each 16-lane group source lane L reads 4 dims of
-        // key k0 + L/4 and lane i receives dim n0 + i of keys k0 .. k0 + 3
-        // (the fragments of a dim block are read while the one before is multiplied)
-        const int r0 = 4 * hh + ((lane & 15) >> 2);
-        auto read_v = [&](int db, bf16x8_t (&a)[4]) {
-          const int ch = db * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-          const char* at = cV + r0 * ROWB + ((ch ^ fv(r0)) * 16) + 8 * (lane & 1);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s16x4 half[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)     // fv repeats every 4 rows
-              half[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (lds_s16x4*)(at + (16 * i + 8 * x) * ROWB));
-            a[i] = __builtin_bit_cast(
-                bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
-          }
-        };
-        bf16x8_t va[2][4];
-        read_v(0, va[0]);
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          if (db + 1 < DB) read_v(db + 1, va[(db + 1) & 1]);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[db & 1][i], pb[i], o[db], 0, 0, 0);
-        }
-        __builtin_amdgcn_s_setprio(0);
+        for (int jj = 0; jj < DPW; ++jj) issue_run(jj, ko, von2, sl);
       }
-      if constexpr (FP8) {
-        if (kb + 1 < nkb) put(u ^ 1);
-      }
-      if constexpr (!FP8) wait_loads();
-      __syncthreads();   // block kb + 1 landed, stage u is free
+      mask = mask1;
+      mask1 = there;
+      vo = von;
+      von = von2;
     }
 
     const float l = l_run + __shfl_xor(l_run, 32, 64);
-    bool ok = finite(l);
+    float zero = l * 0.0f;             // NaN where l or an o is not finite
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) ok &= finite(o[i][v]);
-    const uint64_t bad = __ballot(valid && !ok);
+      for (int v = 0; v < 16; ++v) zero = fmaf(o[i][v], 0.0f, zero);
+    const uint64_t bad = __ballot(valid && zero != 0.0f);
     const uint32_t redo = (uint32_t)bad | (uint32_t)(bad >> 32);   // by column
     float* pp = nullptr;     // this column's partial result: m, l, then the dims
-    if (!whole) pp = part + (((int64_t)(nt - 1 - ti) * c.n_kv_heads + hk) * parts + p) * TC_ * (HD + 2);
-    if (valid && !((redo >> c32) & 1)) {
+    if (!whole) pp = part + (((int64_t)ti * c.n_kv_heads + hk) * parts + p) * TC_ * (HD + 2);
+    if (whole) {
+      // turned round in LDS (the wave's own 32 rows, chunk c of row r at c ^ f(r)),
+      // so that whole rows are written
+      __syncthreads();                 // V is read
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      char* row = &sV[0][0] + (wave * 32 + c32) * ROWB;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int v = 0; v < 16; v += 4) {
-          const int d = db * 32 + 2 * v + 4 * hh;
-          if (whole) {
-            *reinterpret_cast<uint2*>(out + qat + d) =
-                make_uint2(pack_bf16x2(o[db][v] * inv, o[db][v + 1] * inv),
-                           pack_bf16x2(o[db][v + 2] * inv, o[db][v + 3] * inv));
-          } else {
-            *reinterpret_cast<float4*>(pp + TC_ * 2 + j * HD + d) =
-                make_float4(o[db][v], o[db][v + 1], o[db][v + 2], o[db][v + 3]);
-          }
-        }
-      if (!whole && hh == 0) *reinterpret_cast<float2*>(pp + 2 * j) = make_float2(m_ref, l);
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<uint2*>(row + ((db * 4 + v / 4) ^ (c32 & (NCO - 1))) * 16 + 8 * hh) =
+              make_uint2(pack_bf16x2(o[db][v] * inv, o[db][v + 1] * inv),
+                         pack_bf16x2(o[db][v + 2] * inv, o[db][v + 3] * inv));
+#pragma unroll
+      for (int i = 0; i < 32 * NCO / 64; ++i) {
+        const int r = i * (64 / NCO) + lane / NCO, ch = lane % NCO;
+        const int64_t at = __shfl((long long)qat, r, 64);
+        const uint4 y = *reinterpret_cast<const uint4*>(
+            &sV[0][0] + (wave * 32 + r) * ROWB + (ch ^ (r & (NCO - 1))) * 16);
+        if (wave * 32 + r < tile.cols && !((redo >> r) & 1))
+          *reinterpret_cast<uint4*>(out + at + ch * 8) = y;
+      }
+    } else if (valid && !((redo >> c32) & 1)) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<float4*>(pp + TC_ * 2 + j * HD + db * 32 + 2 * v + 4 * hh) =
+              make_float4(o[db][v], o[db][v + 1], o[db][v + 2], o[db][v + 3]);
+      if (hh == 0) *reinterpret_cast<float2*>(pp + 2 * j) = make_float2(m_ref, l);
     }
     for (uint32_t left = redo; left; left &= left - 1) {
       const int x = __ffs(left) - 1, jj = wave * 32 + x;
@@ -680,7 +792,7 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(
     T* __restrict__ out) {
   constexpr int CPB = 256 / (HD / 4);      // columns of a workgroup
   const int ti = blockIdx.x, hk = blockIdx.y, nt = *n_tiles;
-  if (ti >= nt || nt > max_tiles) return;
+  if (ti >= nt || nt > max_tiles) return;      // (more: nothing was cut)
   const Tile tile = tiles[ti];
   const int G = H / n_kv_heads;
   const int j = blockIdx.z * CPB + threadIdx.x / (HD / 4), d = threadIdx.x % (HD / 4) * 4;
@@ -722,8 +834,9 @@ constexpr int KB32 = 32;
 template <int HD, bool FP8>
 __global__ __launch_bounds__(kTile32Threads) void paged_tile_f32_kernel(
     int H, float scale_log2, const float* __restrict__ q, Entries e, PagedView c,
-    const Tile* __restrict__ tiles, const int32_t* __restrict__ n_tiles, int max_tiles, int parts,
-    float* __restrict__ out, float* __restrict__ part) {
+    const Tile* __restrict__ tiles, const int32_t* __restrict__ n_tiles,
+    int max_tiles, int parts, float* __restrict__ out,
+    float* __restrict__ part) {
   constexpr int DB = HD / 16;
   constexpr int ROW = HD;                            // floats of a row in LDS
   constexpr int NCH = HD * (FP8 ? 1 : 4) / 16;       // 16-byte pieces of a cache row
@@ -744,18 +857,16 @@ __global__ __launch_bounds__(kTile32Threads) void paged_tile_f32_kernel(
   auto fv = [](int r) { return 4 * ((r >> 2) & 3); };
 
   for (int ti = it.tile; ti < nt; ti += max_tiles) {
-    const Tile tile = tiles[nt - 1 - ti];
+    const Tile tile = tiles[ti];
+    if (tile.cols == 0) return;
     const int32_t* pages = c.table + (int64_t)tile.seq * c.max_pages;
-    const int tend = tile_end(e, c, tile, G, hk);
     const int j = wave * 16 + c16;
     const bool valid = j < tile.cols;
-    int qk, qh, qlim = 0;
+    int qk, qh;
     column_of(tile, valid ? j : 0, G, hk, &qk, &qh);
     const int64_t qat = ((int64_t)qk * H + qh) * HD;
-    if (valid) {
-      int b;
-      qlim = entry_limit(e, c, e.rows[qk], &b);
-    }
+    int tend;
+    const int qlim = tile_limits(e, c, tile, G, hk, j, &tend);
     int wend = qlim;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) wend = max(wend, __shfl_xor(wend, o, 64));
@@ -904,7 +1015,7 @@ __global__ __launch_bounds__(kTile32Threads) void paged_tile_f32_kernel(
     bad |= bad >> 32;
     const uint32_t redo = (uint32_t)(bad | (bad >> 16)) & 0xffffu;
     float* pp = nullptr;
-    if (!whole) pp = part + (((int64_t)(nt - 1 - ti) * c.n_kv_heads + hk) * parts + p) * TC_ * (HD + 2);
+    if (!whole) pp = part + (((int64_t)ti * c.n_kv_heads + hk) * parts + p) * TC_ * (HD + 2);
     if (valid && !((redo >> c16) & 1)) {
       const float f = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
       float* dst = whole ? out + qat : pp + TC_ * 2 + j * HD;
@@ -1423,8 +1534,9 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
     float* part = (float*)(w + ts.off_part);
     const int64_t items = (int64_t)ts.max_tiles * kv->n_kv_heads * ts.parts;
     ADEPT_REQUIRE(items <= 1 << 23, "paged_attend: too many entries");
-    ADEPT_LAUNCH(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, e, n_heads / kv->n_kv_heads,
-                 (int32_t*)(w + ts.off_starts), tiles, n_tiles);
+    ADEPT_LAUNCH(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, e,
+                 n_heads / kv->n_kv_heads, ts.max_tiles, (int32_t*)(w + ts.off_starts), tiles,
+                 n_tiles);
     ADEPT_CHECK_LAUNCH("paged_plan");
     const dim3 grid((unsigned)((items + 7) / 8 * 8));
 #define ADEPT_TILE(KERNEL, T, HD, FP8, THREADS)                                                  \
