@@ -373,23 +373,44 @@ def _need(cond, what, why):
         raise AdeptError(f"{what}: {why}")
 
 
-def _need_here(what, *tensors):
-    """Tensors on the current device (the library launches on its streams)."""
-    here = None
-    for t in tensors:
-        if t is not None:
-            at = t.get_device()
-            if at < 0 or (here is not None and at != here):
-                raise AdeptError(f"{what}: tensors must be on the current HIP device")
-            here = at
-    if here != torch.cuda.current_device():
-        raise AdeptError(f"{what}: tensors must be on the current HIP device")
+def _elsewhere(what):
+    return AdeptError(f"{what}: tensors must be on the current HIP device")
 
 
-def _need_i32(what, *tensors):
+def _ptrs(what, dev, *tensors):
+    """Pointers of tensors (None: NULL) on device `dev`."""
+    out = []
     for t in tensors:
-        if t is not None and not (t.dtype is torch.int32 and t.is_contiguous()):
+        if t is None:
+            out.append(None)
+        elif t.get_device() == dev:
+            out.append(t.data_ptr())
+        else:
+            raise _elsewhere(what)
+    return out
+
+
+def _i32_ptrs(what, dev, *tensors):
+    """The same of contiguous int32 tensors."""
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+        elif t.dtype is not torch.int32 or not t.is_contiguous():
             raise AdeptError(f"{what}: index tensors must be contiguous int32")
+        elif t.get_device() == dev:
+            out.append(t.data_ptr())
+        else:
+            raise _elsewhere(what)
+    return out
+
+
+def _device_of(what, kv):
+    """The cache's device, which has to be the current one (the library launches on its streams)."""
+    dev = kv.tensors[0].get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise _elsewhere(what)
+    return dev
 
 
 def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
@@ -399,6 +420,8 @@ def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
     _need(k.dim() == 3 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in _KV_TYPES and
           k.is_contiguous() and v.is_contiguous(),
           "paged_kv", "k and v must be contiguous [n_slots, Hkv, hd] of one cache type")
+    for t in (v, k_scale, v_scale):
+        _need(t is None or t.device == k.device, "paged_kv", "one device for the whole cache")
     _need(page_size >= 1 and k.shape[0] % page_size == 0,
           "paged_kv", f"{k.shape[0]} slots are no multiple of the page size {page_size}")
     fp8 = _KV_TYPES[k.dtype] == KV_FP8
@@ -413,45 +436,51 @@ def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
     return kv
 
 
-def _paged_rows(what, kv, k, v):
-    heads, hd = kv.n_kv_heads, kv.head_dim
-    for t in (k, v):
-        if not (t.dim() == 3 and t.shape[1] == heads and t.shape[2] == hd and t.dtype is k.dtype and
-                t.dtype in (torch.float32, torch.bfloat16) and
-                (t.shape[0] == 0 or (t.stride(2) == 1 and t.stride(1) == hd))):
-            raise AdeptError(f"{what}: rows must be f32 or bf16 [n, {heads}, {hd}] with contiguous "
-                             "heads")
-
-
-def _row_stride(t):
-    """Elements between the rows of [n, H, hd] (of one row or none: any)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+def _rows(what, kv, dev, t, dtype):
+    """Pointer and row stride of K or V rows [n, Hkv, hd] with contiguous heads."""
+    n, heads, hd = t.shape if t.dim() == 3 else (0, 0, 0)
+    row = heads * hd
+    if heads != kv.n_kv_heads or hd != kv.head_dim or t.dtype is not dtype or (
+            dtype is not torch.bfloat16 and dtype is not torch.float32):
+        raise AdeptError(f"{what}: rows must be f32 or bf16 [n, {kv.n_kv_heads}, {kv.head_dim}]")
+    if n > 1 or not t.is_contiguous():
+        r, h, d = t.stride()
+        if n and (d != 1 or (heads > 1 and h != hd)):
+            raise AdeptError(f"{what}: the heads of a row must be contiguous")
+        row = r if n > 1 else row
+    if t.get_device() != dev:
+        raise _elsewhere(what)
+    return t.data_ptr(), row
 
 
 def paged_store(kv, k, v, slot, rows=None, n_rows=None, stream=None):
     """Rows of k, v [n, Hkv, hd] (any row stride) into the slots slot[row] of the cache, quantised
     if it is an 8-bit one; rows: the listed rows only, n_rows (device int32 [1]): how many of
     them."""
-    _paged_rows("paged_store", kv, k, v)
-    _need_here("paged_store", *kv.tensors, k, v, slot, rows, n_rows)
-    _need_i32("paged_store", slot, rows, n_rows)
-    _need(k.shape[0] == v.shape[0] == slot.numel(), "paged_store", "one slot for each row")
-    n = k.shape[0] if rows is None else rows.numel()
-    _check(lib().adept_paged_store(dtype_code(k), ctypes.byref(kv), ptr(k), _row_stride(k), ptr(v),
-                                   _row_stride(v), ptr(rows), ptr(n_rows), n, ptr(slot),
+    dev = _device_of("paged_store", kv)
+    kp, ks = _rows("paged_store", kv, dev, k, k.dtype)
+    vp, vs = _rows("paged_store", kv, dev, v, k.dtype)
+    sp, rp, np_ = _i32_ptrs("paged_store", dev, slot, rows, n_rows)
+    n = k.shape[0]
+    if v.shape[0] != n or slot.numel() != n:
+        raise AdeptError("paged_store: one slot for each row")
+    if rows is not None:
+        n = rows.numel()
+    _check(lib().adept_paged_store(dtype_code(k), ctypes.byref(kv), kp, ks, vp, vs, rp, np_, n, sp,
                                    stream_handle(stream)), "adept_paged_store")
 
 
 def paged_load(kv, slot, k, v, n_rows=None, stream=None):
     """k[i], v[i] = the cache's values at slot[i] (k, v [n, Hkv, hd], any row stride)."""
-    _paged_rows("paged_load", kv, k, v)
-    _need_here("paged_load", *kv.tensors, k, v, slot, n_rows)
-    _need_i32("paged_load", slot, n_rows)
+    dev = _device_of("paged_load", kv)
+    kp, ks = _rows("paged_load", kv, dev, k, k.dtype)
+    vp, vs = _rows("paged_load", kv, dev, v, k.dtype)
+    sp, np_ = _i32_ptrs("paged_load", dev, slot, n_rows)
     n = slot.numel()
-    _need(k.shape[0] >= n and v.shape[0] >= n, "paged_load", "fewer output rows than slots")
-    _check(lib().adept_paged_load(dtype_code(k), ctypes.byref(kv), ptr(slot), ptr(n_rows), n, ptr(k),
-                                  _row_stride(k), ptr(v), _row_stride(v), stream_handle(stream)),
-           "adept_paged_load")
+    if k.shape[0] < n or v.shape[0] < n:
+        raise AdeptError("paged_load: fewer output rows than slots")
+    _check(lib().adept_paged_load(dtype_code(k), ctypes.byref(kv), sp, np_, n, kp, ks, vp, vs,
+                                  stream_handle(stream)), "adept_paged_load")
 
 
 def paged_attend_workspace_bytes(kv, n_heads, max_active, n_seq, max_pages):
@@ -463,28 +492,29 @@ def paged_attend(kv, q, rows, n_active, max_active, pos, seq, n_seq, page_table,
                  key_len=None, key_live=None, workspace=None, scale=None, stream=None):
     """Attention of the entries q [max_active, H, hd] over the paged cache kv; page_table int32
     [n_seq, max_pages].  workspace: uint8, paged_attend_workspace_bytes()."""
-    H, hd = q.shape[1], q.shape[2]
-    _need_here("paged_attend", *kv.tensors, q, rows, n_active, pos, seq, page_table, out, key_len,
-               key_live, workspace)
-    _need_i32("paged_attend", rows, n_active, pos, seq, page_table, key_len)
-    _need(q.is_contiguous() and out.is_contiguous() and out.dtype == q.dtype and
-          q.dtype in (torch.float32, torch.bfloat16) and hd == kv.head_dim and
-          q.shape[0] >= max_active and out.numel() >= max_active * H * hd and
-          rows.numel() >= max_active,
-          "paged_attend", "q and out must be contiguous [max_active, H, hd] of one type")
-    _need(page_table.dim() == 2 and page_table.shape[0] == n_seq,
-          "paged_attend", "page_table must be [n_seq, max_pages]")
-    _need(key_len is None or key_len.numel() == n_seq, "paged_attend", "one key_len for each sequence")
-    _need(key_live is None or (key_live.dtype == torch.uint8 and key_live.is_contiguous() and
-                               key_live.numel() == kv.n_pages * kv.page_size),
-          "paged_attend", "key_live must be uint8, one for each slot")
+    dev = _device_of("paged_attend", kv)
+    n, H, hd = q.shape
+    if not (q.is_contiguous() and out.is_contiguous() and out.dtype is q.dtype and
+            hd == kv.head_dim and n >= max_active and out.numel() >= max_active * H * hd and
+            rows.numel() >= max_active and
+            (q.dtype is torch.bfloat16 or q.dtype is torch.float32)):
+        raise AdeptError("paged_attend: q and out must be contiguous [max_active, H, hd] of one type")
+    if page_table.dim() != 2 or page_table.shape[0] != n_seq:
+        raise AdeptError("paged_attend: page_table must be [n_seq, max_pages]")
+    if key_len is not None and key_len.numel() != n_seq:
+        raise AdeptError("paged_attend: one key_len for each sequence")
+    if key_live is not None and not (key_live.dtype is torch.uint8 and key_live.is_contiguous() and
+                                     key_live.numel() == kv.n_pages * kv.page_size):
+        raise AdeptError("paged_attend: key_live must be uint8, one for each slot")
+    qp, op, lp, wp = _ptrs("paged_attend", dev, q, out, key_live, workspace)
+    rp, ap, pp, sp, tp, np_ = _i32_ptrs("paged_attend", dev, rows, n_active, pos, seq, page_table,
+                                        key_len)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     scale = 1.0 / math.sqrt(hd) if scale is None else scale
     _check(lib().adept_paged_attend(dtype_code(q), ctypes.byref(kv), H, scale, int(bool(causal)),
-                                    ptr(q), ptr(rows), ptr(n_active), max_active, ptr(pos),
-                                    ptr(seq), n_seq, ptr(page_table), page_table.shape[1],
-                                    ptr(key_len), ptr(key_live), ptr(out), ptr(workspace), ws_bytes,
-                                    stream_handle(stream)), "adept_paged_attend")
+                                    qp, rp, ap, max_active, pp, sp, n_seq, tp, page_table.shape[1],
+                                    np_, lp, op, wp, ws_bytes, stream_handle(stream)),
+           "adept_paged_attend")
 
 
 def layer_workspace_bytes(args: LayerArgs):

@@ -288,6 +288,18 @@ __device__ __forceinline__ int lane_here() {
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// (m, l, o) += the same of other keys; m in the exp2 domain.  Parts without keys
+// have l = 0 and o = 0.
+__device__ __forceinline__ void join(float& m, float& l, f32x4_t& o, float m2, float l2, f32x4_t o2) {
+  const float mn = fmaxf(m, m2);
+  const float a = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+  const float b = m2 == mn ? 1.0f : __builtin_amdgcn_exp2f(m2 - mn);
+  m = mn;
+  l = fmaf(b, l2, l * a);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = fmaf(b, o2[i], o[i] * a);
+}
+
 // Column j of a tile: its entry and query head.
 __device__ __forceinline__ void column_of(const Tile& t, int j, int G, int hk, int* k, int* h) {
   const int c = t.col + j;
@@ -798,20 +810,13 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(
   const int j = blockIdx.z * CPB + threadIdx.x / (HD / 4), d = threadIdx.x % (HD / 4) * 4;
   if (j >= tile.cols) return;
   const float* pp = part + ((int64_t)ti * n_kv_heads + hk) * parts * TC_ * (HD + 2);
-  float m = -INFINITY;
-  for (int p = 0; p < parts; ++p) m = fmaxf(m, pp[(int64_t)p * TC_ * (HD + 2) + 2 * j]);
-  float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  float m = -INFINITY, l = 0.0f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int p = 0; p < parts; ++p) {
     const float* x = pp + (int64_t)p * TC_ * (HD + 2);
     const float2 ml = *reinterpret_cast<const float2*>(x + 2 * j);
-    const float4 v = *reinterpret_cast<const float4*>(x + TC_ * 2 + j * HD + d);
-    if (ml.x == -INFINITY && ml.y == 0.0f) continue;    // a part without keys
-    const float w = __builtin_amdgcn_exp2f(ml.x - m);
-    l = fmaf(w, ml.y, l);
-    o[0] = fmaf(w, v.x, o[0]);
-    o[1] = fmaf(w, v.y, o[1]);
-    o[2] = fmaf(w, v.z, o[2]);
-    o[3] = fmaf(w, v.w, o[3]);
+    join(m, l, o, ml.x, ml.y, *reinterpret_cast<const f32x4_t*>(x + TC_ * 2 + j * HD + d));
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   int k, h;
@@ -1047,21 +1052,27 @@ __global__ __launch_bounds__(kTile32Threads) void paged_tile_f32_kernel(
 }
 
 // Tiles that the host counts on, and the parts of the keys with which they make
-// about two workgroups a CU (a part keeps at least 256 of the keys there may be).
+// up to kParts workgroups, two a CU; a part keeps kPartKeys of the keys there may
+// be (1 x 64 tokens over 700, 32/8 heads: 24 us, 29 with 64).  f32 tiles take
+// longer, 2 us for 32 keys, and gain from shorter parts: 2 x 100 tokens over 300
+// 21 us with parts of 64 keys, 35 with 256; one workgroup a CU.
+constexpr int kParts = 512, kPartKeys = 256, kParts32 = 256, kPartKeys32 = 64;
 struct TileShape {
   int max_tiles, cap_tiles, parts;
   size_t off_tiles, off_starts, off_part, bytes;
 };
-TileShape tile_shape(const adept_paged_kv& kv, int n_heads, int max_active, int n_seq,
-                     int max_pages) {
+TileShape tile_shape(adept_dtype dt, const adept_paged_kv& kv, int n_heads, int max_active,
+                     int n_seq, int max_pages) {
   const int64_t G = n_heads / kv.n_kv_heads, keys = (int64_t)max_pages * kv.page_size;
   TileShape t{};
   const int64_t full = max_active * G / TC_;
   t.max_tiles = (int)(full + std::min(n_seq, max_active));
   t.cap_tiles = (int)(full + max_active);
   const int64_t base = (int64_t)t.max_tiles * kv.n_kv_heads;
-  t.parts = (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(base, 1),
-                                                         (keys + 255) / 256, 32}));
+  const bool f32 = dt == ADEPT_F32;
+  t.parts = (int)std::max<int64_t>(
+      1, std::min<int64_t>({(f32 ? kParts32 : kParts) / std::max<int64_t>(base, 1),
+                            ceil_div(keys, f32 ? kPartKeys32 : kPartKeys), 32}));
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   t.off_tiles = 256;
   t.off_starts = t.off_tiles + up((size_t)t.cap_tiles * sizeof(Tile));
@@ -1093,7 +1104,7 @@ struct Stretch {
   int k, part, parts, seq, t0, t1;
 };
 __device__ __forceinline__ Stretch step_stretch(const Entries& e, const PagedView& c, int n, int x,
-                                                int want) {
+                                                int want, int least) {
   constexpr int P = kStepEntries / 256;
   __shared__ long long s_sum[4];
   __shared__ int s_cnt[4], s_out[6];
@@ -1119,7 +1130,7 @@ __device__ __forceinline__ Stretch step_stretch(const Entries& e, const PagedVie
   if (tid < 6) s_out[tid] = 0;
   __syncthreads();
   sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-  const int cut = (int)max((sum + want - 1) / want, 1ll);   // units of a stretch
+  const int cut = (int)max((sum + want - 1) / want, (long long)least);   // units of a stretch
   int cnt = 0;
 #pragma unroll
   for (int i = 0; i < P; ++i)
@@ -1169,7 +1180,7 @@ __device__ __forceinline__ Stretch step_stretch(const Entries& e, const PagedVie
 // needed (64 sequences of 4096 keys in 8 bits: 477 us, 756 where the slots were
 // formed at once, which waits for every load before).
 template <int HD, bool FP8>
-__global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kernel(int H, int col_groups, int want,
+__global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kernel(int H, int col_groups, int want, int least,
                                                          float scale_log2,
                                                          const bf16* __restrict__ q, Entries e,
                                                          PagedView c, bf16* __restrict__ out,
@@ -1188,7 +1199,7 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
   const int x = blockIdx.x % items, hk = blockIdx.x / items % c.n_kv_heads,
             cg = blockIdx.x / items / c.n_kv_heads;
   const int n = min(*e.n_active, e.max_active);
-  const Stretch st = step_stretch(e, c, n, x, want);
+  const Stretch st = step_stretch(e, c, n, x, want, least);
   if (st.parts == 0) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1388,43 +1399,59 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
   if (tid == 0 && st.part == 0 && hk == 0 && cg == 0) spans[st.k] = make_int2(x, st.parts);
 }
 
-// Joins the stretches of each entry that has several.
+// Joins the stretches of each entry that has several: a workgroup per (entry,
+// head), whose groups of HD/4 threads (four dims a thread) take every PG-th stretch
+// each and meet in LDS.  (One group for all stretches: 30 us for 126 of them.)
 template <int HD>
 __global__ __launch_bounds__(256) void paged_step_join_kernel(int H, Entries e,
                                                               const int2* __restrict__ spans,
                                                               const float* __restrict__ part,
                                                               bf16* __restrict__ out) {
-  constexpr int CPB = 256 / (HD / 4);
-  const int k = blockIdx.x, n = min(*e.n_active, e.max_active);
-  const int h = blockIdx.y * CPB + threadIdx.x / (HD / 4), d = threadIdx.x % (HD / 4) * 4;
-  if (k >= n || h >= H) return;
+  constexpr int PG = 256 / (HD / 4);
+  __shared__ float s_m[PG], s_l[PG];
+  __shared__ __attribute__((aligned(16))) float s_o[PG][HD];
+  const int k = blockIdx.x, h = blockIdx.y, n = min(*e.n_active, e.max_active);
+  if (k >= n) return;
   const int2 sp = spans[k];
   if (sp.y <= 1) return;
-  const float* pp = part + ((int64_t)sp.x * H + h) * (HD + 4);
+  const int pg = threadIdx.x / (HD / 4), d = threadIdx.x % (HD / 4) * 4;
   const int64_t step = (int64_t)H * (HD + 4);
-  float m = -INFINITY;
-#pragma unroll 4
-  for (int p = 0; p < sp.y; ++p) m = fmaxf(m, pp[p * step]);
-  float l = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int p = 0; p < sp.y; ++p) {
-    const float2 ml = *reinterpret_cast<const float2*>(pp + p * step);
-    const float4 v = *reinterpret_cast<const float4*>(pp + p * step + 4 + d);
-    const float f = ml.x == m ? 1.0f : __builtin_amdgcn_exp2f(ml.x - m);
-    l = fmaf(f, ml.y, l);
-    y[0] = fmaf(f, v.x, y[0]);
-    y[1] = fmaf(f, v.y, y[1]);
-    y[2] = fmaf(f, v.z, y[2]);
-    y[3] = fmaf(f, v.w, y[3]);
+  const float* pp = part + ((int64_t)sp.x * H + h) * (HD + 4);
+  float m = -INFINITY, l = 0.0f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 4;
+  for (int p0 = pg; p0 < sp.y; p0 += U * PG) {
+    float2 ml[U];
+    f32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float* x = pp + min(p0 + u * PG, sp.y - 1) * step;
+      ml[u] = *reinterpret_cast<const float2*>(x);
+      v[u] = *reinterpret_cast<const f32x4_t*>(x + 4 + d);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p0 + u * PG >= sp.y) break;
+      join(m, l, o, ml[u].x, ml[u].y, v[u]);
+    }
   }
+  if (d == 0) {
+    s_m[pg] = m;
+    s_l[pg] = l;
+  }
+  *reinterpret_cast<f32x4_t*>(&s_o[pg][d]) = o;
+  __syncthreads();
+  if (pg != 0) return;
+  for (int x = 1; x < PG; ++x)
+    join(m, l, o, s_m[x], s_l[x], *reinterpret_cast<const f32x4_t*>(&s_o[x][d]));
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  *reinterpret_cast<uint2*>(out + ((int64_t)k * H + h) * HD + d) =
-      make_uint2(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv));
+  store4(out + ((int64_t)k * H + h) * HD + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
 
-// want: stretches of the call's keys for each (K/V head, column group)
+// want: stretches of the call's keys for each (K/V head, column group); least:
+// units of a stretch at least
 struct StepShape {
-  int groups, want, items;
+  int groups, want, least, items;
   bool cut;          // whether an entry can have several stretches
   size_t off_part, bytes;
 };
@@ -1434,8 +1461,14 @@ StepShape step_shape(const adept_paged_kv& kv, int n_heads, int max_active, int 
   t.groups = ceil_div(G, SC);
   const int64_t keys = (int64_t)max_pages * kv.page_size;
   t.want = std::max(1, kStepItems / (kv.n_kv_heads * t.groups));
-  t.cut = keys > kStepUnit;
-  const int64_t most = std::max<int64_t>(1, (keys + kStepUnit - 1) / kStepUnit);
+  // A stretch has at least so many units.  Four where the entries alone fill the
+  // card (64 sequences of up to 300 keys, 8 K/V heads: 15 us, 27 with one), two
+  // where single units would be over 512 workgroups (16 of 1000: 19 us, 23; one of
+  // 16000: 16 us, 22), else one (one of 700, 32 heads: 10 us, 12 with two).
+  const int64_t base = (int64_t)max_active * kv.n_kv_heads * t.groups;
+  t.least = base >= 256 ? 4 : base * ceil_div(keys, kStepUnit) > 512 ? 2 : 1;
+  t.cut = keys > t.least * kStepUnit;
+  const int64_t most = std::max<int64_t>(1, ceil_div(keys, t.least * kStepUnit));
   t.items = (int)std::min<int64_t>((int64_t)max_active + t.want, max_active * most);
   t.off_part = ((size_t)max_active * sizeof(int2) + 255) & ~(size_t)255;
   t.bytes = t.off_part;
@@ -1460,7 +1493,8 @@ extern "C" size_t adept_paged_attend_workspace_bytes(const adept_paged_kv* kv, i
   if (!kv || kv->n_kv_heads <= 0 || n_heads < kv->n_kv_heads || max_active < 0 || n_seq <= 0 ||
       max_pages <= 0)
     return 256;
-  return std::max(tile_shape(*kv, n_heads, max_active, n_seq, max_pages).bytes,
+  return std::max(std::max(tile_shape(ADEPT_F32, *kv, n_heads, max_active, n_seq, max_pages).bytes,
+                           tile_shape(ADEPT_BF16, *kv, n_heads, max_active, n_seq, max_pages).bytes),
                   step_shape(*kv, n_heads, max_active, max_pages).bytes);
 }
 
@@ -1507,7 +1541,7 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
     ADEPT_REQUIRE(items <= 1 << 23, "paged_attend: too many entries");
 #define ADEPT_STEP(HD, FP8)                                                                       \
   ADEPT_LAUNCH((paged_step_kernel<HD, FP8>), dim3((unsigned)items), dim3(256), 0, s, n_heads,     \
-               ss.groups, ss.want, sl, (const bf16*)q, e, c, (bf16*)out, spans, part)
+               ss.groups, ss.want, ss.least, sl, (const bf16*)q, e, c, (bf16*)out, spans, part)
     if (hd == 128) {
       if (fp8) ADEPT_STEP(128, true); else ADEPT_STEP(128, false);
     } else {
@@ -1516,7 +1550,7 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
 #undef ADEPT_STEP
     ADEPT_CHECK_LAUNCH("paged_step");
     if (ss.cut) {
-      const dim3 jg(max_active, ceil_div(n_heads, 1024 / hd));
+      const dim3 jg(max_active, n_heads);
       if (hd == 128)
         ADEPT_LAUNCH(paged_step_join_kernel<128>, jg, dim3(256), 0, s, n_heads, e, spans, part,
                      (bf16*)out);
@@ -1527,7 +1561,7 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
     return launch_status("paged_attend");
   }
   if (tiles_fit(*kv)) {
-    const TileShape ts = tile_shape(*kv, n_heads, max_active, n_seq, max_pages);
+    const TileShape ts = tile_shape(dt, *kv, n_heads, max_active, n_seq, max_pages);
     char* w = (char*)workspace;
     int32_t* n_tiles = (int32_t*)w;
     Tile* tiles = (Tile*)(w + ts.off_tiles);
