@@ -399,6 +399,11 @@ adept_status adept_paged_load(adept_dtype dt, const adept_paged_kv* kv, const in
  *  sums in f32; zeros for an entry that sees no key (or whose sequence is
  *  outside 0 .. n_seq-1).  What is left out has no influence, whatever it holds.
  *  Entries behind the last active one are left as they were.
+ *  Where max_active <= n_seq every entry reads its keys for itself (one new token
+ *  per sequence); else the entries of a sequence share them in tiles.  So a call
+ *  for the many tokens of a few sequences names those (their rows of the page
+ *  table, n_seq of them), not a whole table.  At most about 2^23 (entry, K/V head)
+ *  pairs, else ADEPT_E_INVALID.
  *  workspace: adept_paged_attend_workspace_bytes() bytes, 16-byte aligned; its
  *  contents on entry do not matter.  Calls that may overlap need their own. */
 size_t adept_paged_attend_workspace_bytes(const adept_paged_kv* kv, int n_heads, int max_active,

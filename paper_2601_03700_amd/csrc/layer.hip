@@ -266,36 +266,53 @@ adept_status kv_generate_family(const adept_layer_args* a, int max_skipped, adep
                           ws.kvgen_bytes, stream);
 }
 
-// Step 3: attention over the mixed cache.  Over an FP8 cache the layer's K/V of
-// all rows of the pass are quantised into their slots first: those of the active
+// The paged cache of one layer, whose K/V over the other types are at kc, vc.
+adept_paged_kv layer_kv(const adept_layer_args* a, const PagedStep* pg, int layer, const void* kc,
+                        const void* vc) {
+  adept_paged_kv kv = *pg->kv;
+  const int64_t slots = (int64_t)(layer - 1) * paged_slots(kv);
+  if (kv.dtype == ADEPT_KV_FP8) {
+    kv.k = (uint8_t*)kv.k + slots * a->n_heads * a->head_dim;
+    kv.v = (uint8_t*)kv.v + slots * a->n_heads * a->head_dim;
+    kv.k_scale += slots * a->n_heads;
+    kv.v_scale += slots * a->n_heads;
+  } else {
+    kv.k = (void*)kc;
+    kv.v = (void*)vc;
+  }
+  return kv;
+}
+
+// Over an FP8 cache, before the attention and also where no row is left to attend:
+// the layer's K/V of all rows of the pass into their slots.  Those of the active
 // rows the QKV GEMM has just written, those of the rows that exited before were
 // generated after their exit or by that GEMM.
+adept_status store_step(const adept_layer_args* a, const PagedStep* pg, int layer, const void* kc,
+                        const void* vc, hipStream_t s) {
+  if (!pg || pg->kv->dtype != ADEPT_KV_FP8) return ADEPT_OK;
+  const adept_paged_kv kv = layer_kv(a, pg, layer, kc, vc);
+  const int64_t dq = (int64_t)a->n_heads * a->head_dim;
+  return adept_paged_store((adept_dtype)a->dtype, &kv, kc, dq, vc, dq, nullptr, nullptr, a->n_tok,
+                           pg->cache_slot, s);
+}
+
+// Step 3: attention over the mixed cache.
 adept_status attend_step(const adept_layer_args* a, const PagedStep* pg, int layer, const void* kc,
                          const void* vc, const int32_t* act, const int32_t* nact,
                          const LayerWs& ws, hipStream_t s) {
   const adept_dtype dt = (adept_dtype)a->dtype;
-  const int H = a->n_heads, hd = a->head_dim, dq = H * hd;
+  const int H = a->n_heads, hd = a->head_dim;
   const float scale = 1.0f / sqrtf((float)hd);
   if (!pg)
     return attend_dispatch(dt, H, hd, scale, 1, a->q_buf, act, nact, a->max_active, a->pos, a->seq,
                            a->n_seq, kc, vc, a->s_max, nullptr, nullptr, a->attn_out, ws.attend,
                            ws.attend_bytes, a->attn_tiles != 0, s);
-  adept_paged_kv kv = *pg->kv;
-  const int64_t slots = (int64_t)(layer - 1) * paged_slots(kv);
-  if (kv.dtype == ADEPT_KV_FP8) {
-    kv.k = (uint8_t*)kv.k + slots * dq;
-    kv.v = (uint8_t*)kv.v + slots * dq;
-    kv.k_scale += slots * H;
-    kv.v_scale += slots * H;
-    ADEPT_TRY(adept_paged_store(dt, &kv, kc, dq, vc, dq, nullptr, nullptr, a->n_tok, pg->cache_slot,
-                                s));
-  } else {
-    kv.k = (void*)kc;
-    kv.v = (void*)vc;
-  }
-  return adept_paged_attend(dt, &kv, H, scale, 1, a->q_buf, act, nact, a->max_active, a->pos, a->seq,
-                            a->n_seq, pg->table, pg->max_pages, nullptr, nullptr, a->attn_out,
-                            ws.attend, ws.attend_bytes, s);
+  ADEPT_TRY(store_step(a, pg, layer, kc, vc, s));
+  const adept_paged_kv kv = layer_kv(a, pg, layer, kc, vc);
+  return paged_attend_dispatch(dt, &kv, H, scale, 1, a->q_buf, act, nact, a->max_active, a->pos,
+                               a->seq, a->n_seq, pg->table, pg->max_pages, nullptr, nullptr,
+                               a->attn_out, ws.attend, ws.attend_bytes,
+                               a->attn_tiles ? kPagedTiles : kPagedSteps, s);
 }
 
 adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* pg, void* stream);
@@ -603,6 +620,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     ADEPT_TRY(exit_in_epilogue(gd));
     ADEPT_TRY(run_gemm(dt, gd, ws.gemm_tmp, s));
   }
+  if (qmax <= 0) ADEPT_TRY(store_step(a, pg, layer, kc, vc, s));
   if (tail) {
     // 8. + 9. exit test and active-list update
     ExitCompact x{};

@@ -60,6 +60,16 @@ constexpr int kMaxEntries = 1 << 23;   // rows or entries of a call (its grid's 
 // slots of a cache and tokens of a sequence: a few blocks past them stay an int
 constexpr int64_t kMaxTokens = INT_MAX - 1023;
 inline int64_t paged_slots(const adept_paged_kv& kv) { return (int64_t)kv.n_pages * kv.page_size; }
+// adept_paged_attend with the kernels named: those for one entry per sequence, for
+// many, or (kPagedAny) by the counts
+enum PagedKernels { kPagedAny = 0, kPagedSteps = 1, kPagedTiles = 2 };
+adept_status paged_attend_dispatch(adept_dtype dt, const adept_paged_kv* kv, int n_heads, float scale,
+                                   int causal, const void* q, const int32_t* rows,
+                                   const int32_t* n_active, int max_active, const int32_t* pos,
+                                   const int32_t* seq, int n_seq, const int32_t* page_table,
+                                   int max_pages, const int32_t* key_len, const uint8_t* key_live,
+                                   void* out, void* workspace, size_t workspace_bytes,
+                                   PagedKernels kernels, hipStream_t s);
 // the checks of a cache descriptor; `what` names the entry point
 adept_status paged_check(const char* what, adept_dtype dt, const adept_paged_kv* kv);
 

@@ -1450,6 +1450,7 @@ __global__ __launch_bounds__(256) void paged_step_join_kernel(int H, Entries e,
 
 // want: stretches of the call's keys for each (K/V head, column group); least:
 // units of a stretch at least
+constexpr int64_t kMaxItems = (1 << 23) - 8;   // workgroups (their threads fit 32 bits)
 struct StepShape {
   int groups, want, least, items;
   bool cut;          // whether an entry can have several stretches
@@ -1478,11 +1479,6 @@ StepShape step_shape(const adept_paged_kv& kv, int n_heads, int max_active, int 
   t.bytes = std::max<size_t>(t.bytes, 256);
   return t;
 }
-// one entry per sequence at most, on average: each reads its keys for itself
-bool step_fits(adept_dtype dt, const adept_paged_kv& kv, int max_active, int n_seq) {
-  return dt == ADEPT_BF16 && tiles_fit(kv) && max_active <= n_seq;
-}
-
 }  // namespace
 }  // namespace adept
 
@@ -1498,14 +1494,15 @@ extern "C" size_t adept_paged_attend_workspace_bytes(const adept_paged_kv* kv, i
                   step_shape(*kv, n_heads, max_active, max_pages).bytes);
 }
 
-extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv* kv, int n_heads,
-                                           float scale, int causal, const void* q,
-                                           const int32_t* rows, const int32_t* n_active,
-                                           int max_active, const int32_t* pos, const int32_t* seq,
-                                           int n_seq, const int32_t* page_table, int max_pages,
-                                           const int32_t* key_len, const uint8_t* key_live,
-                                           void* out, void* workspace, size_t workspace_bytes,
-                                           void* stream) {
+namespace adept {
+
+adept_status paged_attend_dispatch(adept_dtype dt, const adept_paged_kv* kv, int n_heads, float scale,
+                                   int causal, const void* q, const int32_t* rows,
+                                   const int32_t* n_active, int max_active, const int32_t* pos,
+                                   const int32_t* seq, int n_seq, const int32_t* page_table,
+                                   int max_pages, const int32_t* key_len, const uint8_t* key_live,
+                                   void* out, void* workspace, size_t workspace_bytes,
+                                   PagedKernels kernels, hipStream_t s) {
   ADEPT_TRY(paged_check("paged_attend", dt, kv));
   const int hd = kv->head_dim;
   ADEPT_REQUIRE(n_heads > 0 && n_heads <= 4096 && n_heads % kv->n_kv_heads == 0,
@@ -1531,14 +1528,14 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
                     kv->n_pages, shift, kv->n_kv_heads, n_seq};
   const Entries e{rows, n_active, pos, seq, key_len, max_active, causal};
   const float sl = scale * 1.4426950408889634f;   // scores in the exp2 domain
-  hipStream_t s = as_stream(stream);
   const bool fp8 = kv->dtype == ADEPT_KV_FP8;
-  if (step_fits(dt, *kv, max_active, n_seq)) {
+  if (dt == ADEPT_BF16 && tiles_fit(*kv) &&
+      (kernels == kPagedAny ? max_active <= n_seq : kernels == kPagedSteps)) {
     const StepShape ss = step_shape(*kv, n_heads, max_active, max_pages);
     int2* spans = (int2*)workspace;
     float* part = (float*)((char*)workspace + ss.off_part);
     const int64_t items = (int64_t)ss.items * kv->n_kv_heads * ss.groups;
-    ADEPT_REQUIRE(items <= 1 << 23, "paged_attend: too many entries");
+    ADEPT_REQUIRE(items <= kMaxItems, "paged_attend: too many entries");
 #define ADEPT_STEP(HD, FP8)                                                                       \
   ADEPT_LAUNCH((paged_step_kernel<HD, FP8>), dim3((unsigned)items), dim3(256), 0, s, n_heads,     \
                ss.groups, ss.want, ss.least, sl, (const bf16*)q, e, c, (bf16*)out, spans, part)
@@ -1567,7 +1564,7 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
     Tile* tiles = (Tile*)(w + ts.off_tiles);
     float* part = (float*)(w + ts.off_part);
     const int64_t items = (int64_t)ts.max_tiles * kv->n_kv_heads * ts.parts;
-    ADEPT_REQUIRE(items <= 1 << 23, "paged_attend: too many entries");
+    ADEPT_REQUIRE(items <= kMaxItems, "paged_attend: too many entries");
     ADEPT_LAUNCH(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, e,
                  n_heads / kv->n_kv_heads, ts.max_tiles, (int32_t*)(w + ts.off_starts), tiles,
                  n_tiles);
@@ -1616,4 +1613,19 @@ extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv*
   }
 #undef ADEPT_WALK
   return launch_status("paged_attend");
+}
+
+}  // namespace adept
+
+extern "C" adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv* kv, int n_heads,
+                                           float scale, int causal, const void* q,
+                                           const int32_t* rows, const int32_t* n_active,
+                                           int max_active, const int32_t* pos, const int32_t* seq,
+                                           int n_seq, const int32_t* page_table, int max_pages,
+                                           const int32_t* key_len, const uint8_t* key_live,
+                                           void* out, void* workspace, size_t workspace_bytes,
+                                           void* stream) {
+  return paged_attend_dispatch(dt, kv, n_heads, scale, causal, q, rows, n_active, max_active, pos,
+                               seq, n_seq, page_table, max_pages, key_len, key_live, out, workspace,
+                               workspace_bytes, kPagedAny, as_stream(stream));
 }

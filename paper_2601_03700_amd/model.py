@@ -50,11 +50,12 @@ class PagedKVCache:
     (k, v [N, n_pages * page_size, H, hd]), each sequence up to max_pages of them; kv_dtype:
     "f32", "bf16" or "fp8" (e4m3 codes with a scale byte per slot and head, k_scale, v_scale).
     page_table [n_seq, max_pages] int32 on the device (-1: no page); which pages are free is
-    known on the host."""
+    known on the host.  One page more, which no table names, takes the K/V of tokens that have
+    no place."""
 
     def __init__(self, n_layers, n_heads, head_dim, n_seq, n_pages, page_size, max_pages, kv_dtype,
                  device):
-        dims = (n_layers, n_pages * page_size, n_heads, head_dim)
+        dims = (n_layers, (n_pages + 1) * page_size, n_heads, head_dim)
         tdt = torch.uint8 if kv_dtype == "fp8" else _TORCH_DT[kv_dtype]
         self.k = torch.empty(dims, dtype=tdt, device=device)
         self.v = torch.empty(dims, dtype=tdt, device=device)
@@ -113,11 +114,14 @@ class PagedKVCache:
         self.page_table[seq].fill_(-1)
 
     def slots(self, pos, seq):
-        """Slots (int32) of tokens at pos of sequences seq, both int32 device tensors; -1 where a
-        sequence has no page."""
+        """Slots (int32) of tokens at pos of sequences seq, both int32 device tensors; the last
+        slot of the cache where a sequence has no page."""
         p = pos.long()
-        page = self.page_table[seq.long(), p // self.page_size]
-        return torch.where(page < 0, -1, page * self.page_size + (p % self.page_size).to(torch.int32))
+        at = (p // self.page_size).clamp(0, self.max_pages - 1)
+        page = self.page_table[seq.long(), at]
+        there = (page >= 0) & (p >= 0) & (p < self.s_max)
+        return torch.where(there, page * self.page_size + (p % self.page_size).to(torch.int32),
+                           self.n_slots - 1).to(torch.int32)
 
 
 @dataclasses.dataclass
@@ -369,7 +373,8 @@ class DecoderModel:
     def token_pass(self, ids, pos, seq, cache, cfg, force_layer=None, attn_tiles=True,
                    logit_rows=None, on_layer=None):
         """Run token rows (ids/pos/seq: int32 device tensors [n]) through all layers.  Over a
-        paged cache the rows' pages have to be reserved."""
+        paged cache the rows' pages are reserved before (reserve); the K/V of a row without one
+        are lost."""
         s = self.shape
         n = int(ids.shape[0])
         paged = isinstance(cache, PagedKVCache)

@@ -172,6 +172,56 @@ def test_pages_of_finished_sequences_serve_new_ones():
         model.new_paged_cache(1, 4, kv_dtype="f32")
 
 
+def test_layers_that_no_row_reaches_are_stored_too():
+    """8 bits, every row gone after layer 1 and the caller's bound lowered to 0 from layer 2 on:
+    each later layer still holds the generated K and V."""
+    print("paged model, no row left, 8 bits", flush=True)
+    shape, n_seq, T = LLAMA, 2, 20
+    model = build(shape, "bf16")
+    ids = torch.from_numpy(ai.token_ids(2, shape.vocab, n_seq, T)).to(DEV, torch.int32).view(-1)
+    cache = model.new_paged_cache(n_seq, n_pages=8, page_size=8, kv_dtype="fp8")
+    cache.reserve(T)
+    n = ids.numel()
+    pos = torch.arange(T, dtype=torch.int32, device=DEV).repeat(n_seq)
+    seq = torch.arange(n_seq, dtype=torch.int32, device=DEV).repeat_interleave(T)
+    force = torch.ones(n, dtype=torch.int32, device=DEV)
+    st = model.new_state(n, pos, seq, cache.slots(pos, seq), force)
+    B.embed(n, shape.d_model, shape.vocab, ids, model.embed, st.h[0])
+    B.token_init(n, shape.n_layers, shape.d_model, st.active[0], st.counts, st.exit_layer, st.inertia)
+    args = model.layer_args(st, cache, B.exit_cfg(math.inf, shape.n_layers), True)
+    for i in range(1, shape.n_layers + 1):
+        args.max_active = n if i == 1 else 0
+        B.layer_step_paged(args, cache.kv, cache.page_table, i, st.cache_slot)
+    assert (st.exit_layer == 1).all()
+    at = st.cache_slot.long().cpu()
+    for i in range(shape.n_layers):
+        for new, codes, scale in ((st.new_k, cache.k, cache.k_scale), (st.new_v, cache.v, cache.v_scale)):
+            val, E = R.quantised(new[i].cpu())
+            assert torch.equal(R.cache_values(codes[i].cpu()[at], scale[i].cpu()[at]),
+                               val * R.power(E).unsqueeze(-1))
+
+
+def test_rows_without_a_page():
+    """Rows beyond a sequence's pages: computed, and nothing of another sequence changes."""
+    print("paged model, rows without a page", flush=True)
+    shape = LLAMA
+    model = build(shape, "bf16")
+    cfg = B.exit_cfg(math.inf, shape.n_layers)
+    cache = model.new_paged_cache(2, n_pages=6, page_size=8, max_pages=3)
+    ids = ai.token_ids(3, shape.vocab, 2, 16)
+    model.prefill(ids, cfg, cache=cache)
+    k, v = cache.k.clone(), cache.v.clone()
+    pos = torch.tensor([16, 23, 24, 1000, 3], dtype=torch.int32, device=DEV)
+    seq = torch.tensor([0, 0, 0, 0, 1], dtype=torch.int32, device=DEV)
+    model.token_pass(torch.full((5,), 7, dtype=torch.int32, device=DEV), pos.clamp(max=250), seq,
+                     cache, cfg, None, True, torch.arange(5, device=DEV))
+    own = int(cache.slots(pos[4:], seq[4:]))
+    keep = torch.ones(cache.n_slots, dtype=torch.bool, device=DEV)
+    keep[own] = keep[-1] = False
+    for now, then in ((cache.k, k), (cache.v, v)):     # bits: slots not written yet may hold NaN
+        assert torch.equal(now[:, keep].view(torch.int16), then[:, keep].view(torch.int16))
+
+
 @pytest.mark.parametrize("metric", ["global", "local"])
 def test_exits_by_the_policy_over_an_8_bit_cache(metric):
     """The policy's own exits (no schedule) in a prompt and decode passes over 8 bits."""

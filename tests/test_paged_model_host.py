@@ -16,7 +16,7 @@ def cache(n_seq=3, n_pages=6, page=4, max_pages=4, kv="bf16"):
 
 def test_pages_are_taken_as_sequences_grow_and_given_back():
     c = cache()
-    assert (c.n_slots, c.s_max, c.free_pages) == (24, 16, 6)
+    assert (c.n_slots, c.s_max, c.free_pages) == (28, 16, 6)    # a page more, for no one
     c.reserve({0: 5, 2: 1})
     assert c.free_pages == 3 and (c.page_table >= 0).sum(1).tolist() == [2, 0, 1]
     c.reserve({0: 8})                      # fits the pages it has
@@ -40,10 +40,10 @@ def test_pages_are_taken_as_sequences_grow_and_given_back():
 def test_slots():
     c = cache(page=4)
     c.reserve({0: 6, 1: 3})
-    pos = torch.tensor([0, 5, 2, 7, 9], dtype=torch.int32)
-    seq = torch.tensor([0, 0, 1, 1, 2], dtype=torch.int32)
+    pos = torch.tensor([0, 5, 2, 7, 9, 16, -1], dtype=torch.int32)
+    seq = torch.tensor([0, 0, 1, 1, 2, 0, 0], dtype=torch.int32)
     t = c.page_table
-    want = [int(t[0, 0]) * 4, int(t[0, 1]) * 4 + 1, int(t[1, 0]) * 4 + 2, -1, -1]
+    want = [int(t[0, 0]) * 4, int(t[0, 1]) * 4 + 1, int(t[1, 0]) * 4 + 2] + [27] * 4
     got = c.slots(pos, seq)
     assert got.dtype == torch.int32 and got.tolist() == want
 
@@ -54,7 +54,7 @@ def test_layers_lie_behind_each_other():
         first, second = c.layer_kv(1), c.layer_kv(2)
         e = c.k.element_size()
         assert second.k - first.k == c.n_slots * 2 * 16 * e == second.v - first.v
-        assert first.n_pages == 6 and first.dtype == {"f32": 0, "bf16": 1, "fp8": 2}[kv]
+        assert first.n_pages == 7 and first.dtype == {"f32": 0, "bf16": 1, "fp8": 2}[kv]
         if kv == "fp8":
             assert second.k_scale - first.k_scale == c.n_slots * 2
 
