@@ -369,3 +369,46 @@ def test_chunks_are_written_and_attended_in_turn():
         B.paged_load(kv, slot.to(torch.int32).to(DEV), ko, vo)
         assert torch.equal(ko.double().cpu(), ref[0][slot])
         assert torch.equal(vo.double().cpu(), ref[1][slot])
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("n,bound", [(1025, 1025), (1500, 1500), (1024, 1500), (3, 1500), (0, 1500)])
+def test_long_lists_of_single_tokens(cache, n, bound):
+    """More entries than the cut of long ones counts, and a bound above it with fewer there."""
+    print(f"paged attend, {n} of {bound} single tokens, {cache}", flush=True)
+    lens = [(17 * i) % 90 for i in range(bound)]
+    if 0 < n < 10:
+        lens[0] = 3000
+    c = Case("bf16", cache, 2, 1, 64, 16, [(t, 1, 1) for t in lens], seed=n)
+    c.rows, c.q = c.rows[:n], c.q[:n]
+    c.check(max_active=bound) if n else c.run(max_active=bound)
+
+
+@pytest.mark.parametrize("dt,cache", [("bf16", "fp8"), ("f32", "f32")])
+def test_long_lists_of_chunks(dt, cache):
+    """More entries than one pass of the plan takes, more sequences than a wave has lanes, with
+    one to four tiles each."""
+    print(f"paged attend, 9000 entries, {dt}/{cache}", flush=True)
+    shape = [(3 * b, 30 + (37 * b) % 190, 1) for b in range(72)]
+    c = Case(dt, cache, 2, 1, 64, 32, shape)
+    assert len(c.rows) > 8192
+    c.check(max_active=len(c.rows) + 500)
+
+
+@pytest.mark.parametrize("chunk", [1, 40])
+def test_two_calls_at_once(chunk):
+    """On two streams, each with its workspace: the bits of the calls alone."""
+    print(f"paged attend, two streams, {chunk}", flush=True)
+    cases = [Case("bf16", kind, 4, 2, 128, 16, [(900, chunk, 1), (70, chunk, 1)], seed=s)
+             for s, kind in ((1, "bf16"), (2, "fp8"))]
+    alone = [c.run().clone() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    out = [[], []]
+    for _ in range(5):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                out[i].append(c.run())
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, alone[i]) for x in out[i])
