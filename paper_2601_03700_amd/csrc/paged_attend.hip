@@ -1,10 +1,14 @@
 // Attention of new tokens over a paged cache (adept_paged_attend).
 //
-// Tiles (head_dim 64 / 128): the (entry, query head) pairs that
-// read one K/V head of one sequence are the columns of a matrix; a plan kernel
-// cuts each sequence's columns into tiles of 128.  A workgroup takes one (tile,
-// K/V head) and, where there are too few of those to fill the card, a part of
-// the keys, which a second kernel joins.
+// Tiles (head_dim 64 / 128): the (entry, query head) pairs that read one K/V head
+// of one sequence are the columns of a matrix; a plan kernel cuts each sequence's
+// columns into tiles of 128.  A workgroup takes one (tile, K/V head) and, where
+// there are too few of those to fill the card, a part of the keys, which a second
+// kernel joins.  Bound by the matrix cores and the softmax beside them.
+//
+// Steps (head_dim 64 / 128, bf16, one entry per sequence): a workgroup takes a
+// stretch of one entry's keys for one K/V head; a second kernel joins the
+// stretches of an entry.  Bound by HBM.
 //
 // Walk (other widths): one wave per (entry, head) takes the keys one after
 // another: lane l holds the dims l, l + 64, ... of q and of the running output,
@@ -308,8 +312,7 @@ __device__ __forceinline__ void column_of(const Tile& t, int j, int G, int hk, i
 }
 
 // Work item of a workgroup, head by head: tile (-1: none), K/V head, part of the
-// keys.  The hardware deals workgroups
-// round-robin to the 8 XCDs: with 8 K/V heads or more each XCD takes a run of
+// keys.  The hardware deals workgroups round-robin to the 8 XCDs: with 8 K/V heads or more each XCD takes a run of
 // items, so that the tiles in flight on it share a few heads' K/V in its L2;
 // with fewer heads the items are dealt as they come, which keeps the XCDs evenly
 // loaded.
@@ -379,14 +382,18 @@ __device__ __forceinline__ void part_keys(int n, int parts, int p, int* t0, int*
 // its way while block kb + 1 is computed.  Bound by the SIMDs' instruction issue:
 // a 64-key block of a wave takes some 1900 cycles of its SIMD, 1024 of them matrix
 // instructions, the exponentials 512 and the rest of the softmax about 450.  8
-// prompts of 2048 tokens, 32 heads of 128: 360 us (0.75 PFLOP/s).  A bf16 cache is copied there by
-// direct loads; an 8-bit one goes through registers, where its codes become
-// bf16 with their scale in the conversion itself (exactly).  The slot of key
-// t0 + lane is found by every wave (its page read a block earlier: the wait for
-// it would be one for all loads on their way, 519 us against 451 for 8 prompts of
-// 2048 tokens); its ballot is the mask of
-// the keys that are there, and the others' rows are read from a row of zeros,
-// so that they add nothing whatever the cache holds.
+// prompts of 2048 tokens, 32 heads of 128: 370 us with the plan (0.74 PFLOP/s);
+// 500 tokens over 12000 in 8 bits, 64/8 heads: 161 us with the join (0.83).  Waves
+// of 64 columns, which read each fragment for two products but leave a SIMD one
+// wave: 503 us for the 8 prompts.
+//
+// A bf16 cache is copied to LDS by direct loads; an 8-bit one goes through
+// registers, where its codes become bf16 with their scale in the conversion itself
+// (exactly).  The slot of key t0 + lane is found by every wave from a page read a
+// block earlier (read where it is needed its wait would be one for all loads on
+// their way: 15 % more time when that was measured); its ballot is the mask of the
+// keys that are there, and the others' rows are read from a row of zeros, so that
+// they add nothing whatever the cache holds.
 //
 // Chunk c (16 bytes) of row r lies at c ^ fk(r) in K, c ^ fv(r) in V: the K
 // reads (32 rows, two chunks) and the transposing V reads (4 rows, 4 chunks in
@@ -478,15 +485,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
       for (int jj = 0; jj < DPW; ++jj) {
         const int qd = wave * DPW + jj;
         const uint32_t dst[2] = {ldsK + ko + qd * 1024, ldsV + vo + qd * 1024};
-        {
-          const int l = lane_here(), r = qd * RPI + l / NCH;
-          const int s = __shfl(sl, r, 64);
+        const int l = lane_here(), r = qd * RPI + l / NCH;
+        const int s = __shfl(sl, r, 64);
 #pragma unroll
-          for (int op = 0; op < 2; ++op)
-            load_lds16((s < 0 ? (const char*)kZeroRow : base_of(op, s)) +
-                           ((l % NCH) ^ (op ? fv(r) : fk(r))) * 16,
-                       dst[op]);
-        }
+        for (int op = 0; op < 2; ++op)
+          load_lds16((s < 0 ? (const char*)kZeroRow : base_of(op, s)) +
+                         ((l % NCH) ^ (op ? fv(r) : fk(r))) * 16,
+                     dst[op]);
       }
     };
     // 8-bit: codes and scales to registers, then as bf16 to LDS
@@ -610,7 +615,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
     // the weights of these 32 (scores sc), two exponentials to a product; then these
     // into the output (V at va) beside the maximum of sn, which is returned.  The
     // weights are rounded to bf16 (the sum takes the rounded ones, as the product
-    // does).  run: loads on the way, one pair to a product.
+    // does).  run: loads on the way, one pair to a product.  Of the two waves of a
+    // SIMD the one in a step goes first where the other one converts codes or sets
+    // out (1 x 500 over 8 bits 161 us, 167 without; 5 x 250 heads of 64 22.8, 23.6;
+    // bf16 of 128, whose waves do little else, 370 either way).
     auto step = [&](bool run, uint32_t ka, f32x16_t& sn, uint32_t va, const f32x16_t& sc,
                     uint32_t ko, uint32_t vo) {
       constexpr int AHEAD = 3, EPS = 16 / DS;    // fragments read ahead, weights of a product
@@ -619,6 +627,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
       bf16x8_t a[DS], v[2][2];
 #pragma unroll
       for (int ds = 0; ds < AHEAD; ++ds) a[ds] = read_k(ka, ds);
+      if constexpr (FP8 || HD == 64) __builtin_amdgcn_s_setprio(1);
       uint32_t w[8];
 #pragma unroll
       for (int ds = 0; ds < DS; ++ds) {
@@ -656,6 +665,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
         for (int x = db * (16 / DB); x < (db + 1) * (16 / DB); x += 2)
           m = x == 0 ? fmaxf(sn[0], sn[1]) : max3_raw(m, sn[x], sn[x + 1]);
       }
+      if constexpr (FP8 || HD == 64) __builtin_amdgcn_s_setprio(0);
       return m;
     };
 
@@ -1174,18 +1184,16 @@ __device__ __forceinline__ Stretch step_stretch(const Entries& e, const PagedVie
 // wave has a block in flight (16 KB, 8 KB in 8 bits) while it computes.  (K
 // loaded as operands, 64 bytes of 16 rows at a
 // time, halves of lines: 64 sequences of 4096 keys 770 us, 653 so.)
+// The pages of the block after that are read then too, a whole block before their
+// slots are needed (formed at once, which waits for every load before, 64 sequences
+// of 4096 keys in 8 bits took half as long again; 355 us now, 6 TB/s).
 // The four waves' results are joined in LDS; a stretch that is not all of its
-// entry's keys leaves (m, l, o) for paged_step_join_kernel.  The pages of the
-// block after that are read then too, a whole block before their slots are
-// needed (64 sequences of 4096 keys in 8 bits: 477 us, 756 where the slots were
-// formed at once, which waits for every load before).
+// entry's keys leaves (m, l, o) for paged_step_join_kernel.
 template <int HD, bool FP8>
-__global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kernel(int H, int col_groups, int want, int least,
-                                                         float scale_log2,
-                                                         const bf16* __restrict__ q, Entries e,
-                                                         PagedView c, bf16* __restrict__ out,
-                                                         int2* __restrict__ spans,
-                                                         float* __restrict__ part) {
+__global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kernel(
+    int H, int col_groups, int want, int least, float scale_log2, const bf16* __restrict__ q,
+    Entries e, PagedView c, bf16* __restrict__ out, int2* __restrict__ spans,
+    float* __restrict__ part) {
   constexpr int DS = HD / 32;                      // 32-dim steps of S
   constexpr int DB = HD / 16;                      // 16-dim blocks of O^T
   constexpr int ROWB = HD * 2;                     // bytes of a V row in LDS
