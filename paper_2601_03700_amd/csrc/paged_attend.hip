@@ -383,7 +383,7 @@ __device__ __forceinline__ void part_keys(int n, int parts, int p, int* t0, int*
 // a 64-key block of a wave takes some 1900 cycles of its SIMD, 1024 of them matrix
 // instructions, the exponentials 512 and the rest of the softmax about 450.  8
 // prompts of 2048 tokens, 32 heads of 128: 370 us with the plan (0.74 PFLOP/s);
-// 500 tokens over 12000 in 8 bits, 64/8 heads: 161 us with the join (0.83).  Waves
+// 500 tokens over 7900 in 8 bits, 64/8 heads: 161 us with the join (0.83).  Waves
 // of 64 columns, which read each fragment for two products but leave a SIMD one
 // wave: 503 us for the 8 prompts.
 //
