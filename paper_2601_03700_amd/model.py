@@ -51,7 +51,8 @@ class PagedKVCache:
     "f32", "bf16" or "fp8" (e4m3 codes with a scale byte per slot and head, k_scale, v_scale).
     page_table [n_seq, max_pages] int32 on the device (-1: no page); which pages are free is
     known on the host.  One page more, which no table names, takes the K/V of tokens that have
-    no place."""
+    no place.  A pass over an "fp8" cache holds its own rows' K and V of all layers in the
+    model's type beside it: long prompts are better run in pieces (prefill with start)."""
 
     def __init__(self, n_layers, n_heads, head_dim, n_seq, n_pages, page_size, max_pages, kv_dtype,
                  device):

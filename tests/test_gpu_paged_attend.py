@@ -395,6 +395,13 @@ def test_long_lists_of_chunks(dt, cache):
     c.check(max_active=len(c.rows) + 500)
 
 
+@pytest.mark.parametrize("n_seq", [1023, 1024, 1025, 1200])
+def test_many_sequences_of_two_tokens(n_seq):
+    """Hundreds of short tiles in one call."""
+    print(f"paged attend, {n_seq} sequences of 2 tokens", flush=True)
+    Case("bf16", "bf16", 2, 1, 64, 16, [((5 * b) % 40, 2, 1) for b in range(n_seq)]).check()
+
+
 @pytest.mark.parametrize("chunk", [1, 40])
 def test_two_calls_at_once(chunk):
     """On two streams, each with its workspace: the bits of the calls alone."""
