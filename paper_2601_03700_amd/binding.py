@@ -531,10 +531,17 @@ def layer_paged_workspace_bytes(args: LayerArgs, kv, max_pages):
 
 
 def layer_step_paged(args: LayerArgs, kv, page_table, layer, cache_slot=None, stream=None):
-    """layer_step over a paged cache; kv: paged_kv of its first layer, the others behind it."""
-    _check(lib().adept_layer_step_paged(ctypes.byref(args), ctypes.byref(kv), ptr(page_table),
-                                        page_table.shape[1], ptr(cache_slot), layer,
-                                        stream_handle(stream)), "adept_layer_step_paged")
+    """layer_step over a paged cache; kv: paged_kv of its first layer, the others behind it;
+    page_table int32 [n_seq, max_pages]; cache_slot int32, one for each row (8-bit caches)."""
+    if page_table.dim() != 2 or page_table.shape[0] < args.n_seq:
+        raise AdeptError("layer_step_paged: page_table must be [n_seq, max_pages]")
+    if cache_slot is not None and cache_slot.numel() < args.n_tok:
+        raise AdeptError("layer_step_paged: one slot for each row")
+    dev = _device_of("layer_step_paged", kv)
+    tp, cp = _i32_ptrs("layer_step_paged", dev, page_table, cache_slot)
+    _check(lib().adept_layer_step_paged(ctypes.byref(args), ctypes.byref(kv), tp,
+                                        page_table.shape[1], cp, layer, stream_handle(stream)),
+           "adept_layer_step_paged")
 
 
 def embed(n, d_model, vocab, ids, table, h0, stream=None):

@@ -111,3 +111,13 @@ def test_tensors_elsewhere_are_refused():
         B.paged_load(kv_, i, t(4, 2, 64), t(4, 2, 64))
     with pytest.raises(B.AdeptError, match="device"):
         B.paged_attend(kv_, t(4, 2, 64), i, i, 4, i, i, 1, i.view(1, 4), t(4, 2, 64))
+
+
+@pytest.mark.parametrize("table,slots", [((2, 4), 5), ((3,), 5), ((3, 4), 4), ((3, 4), 5)])
+def test_layer_step_checks_its_tables(table, slots):
+    """Too few rows or slots; the last case fits and is refused for being on the host."""
+    a = B.LayerArgs()
+    a.n_seq, a.n_tok = 3, 5
+    kv_ = B.paged_kv(t(8, 2, 64), t(8, 2, 64), 4)
+    with pytest.raises(B.AdeptError, match="page_table|one slot|current HIP device"):
+        B.layer_step_paged(a, kv_, t(*table, dtype=torch.int32), 1, t(slots, dtype=torch.int32))
