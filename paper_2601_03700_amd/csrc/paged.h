@@ -6,8 +6,10 @@
 namespace adept {
 
 // Scale bytes: 127 + E, -100 <= E <= 100.  Inside that range a code times its
-// scale is a normal bf16 and f32 number and so is the scale's inverse.
+// scale is a normal bf16 and f32 number and so is the scale's inverse.  A slot
+// that was never written may hold any byte: 255 makes every code NaN, 0's too.
 constexpr int kScaleMin = 127 - 100, kScaleMax = 127 + 100;
+constexpr uint8_t kScaleOne = 127;
 __device__ __forceinline__ float scale_of(uint8_t byte) { return __uint_as_float((uint32_t)byte << 23); }
 
 // Two e4m3 codes (the low or the high half of w) times a power of two: exact

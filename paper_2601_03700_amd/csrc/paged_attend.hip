@@ -513,7 +513,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
           } else {
             code[op][i] = *reinterpret_cast<const u32x4_t*>(base_of(op, s) + l % PCH * 16);
             csc[op][i] = sc[(int64_t)s * c.n_kv_heads + hk];
-            if (__shfl(sl, r, 64) < 0) code[op][i] = u32x4_t{0, 0, 0, 0};
+            // not there: zeros, with a scale of their own (0 times slot 0's may be NaN)
+            if (__shfl(sl, r, 64) < 0) {
+              code[op][i] = u32x4_t{0, 0, 0, 0};
+              csc[op][i] = kScaleOne;
+            }
           }
         }
       }
@@ -1241,7 +1245,7 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
   u32x4_t kr[RI], vr[RI];
   uint8_t ksc[RI], vsc[RI];     // scale bytes
   // a key that is not there: slot 0 is read in its place, its score masked and
-  // its V row cleared
+  // its V row cleared, the scale with it (slot 0's may be no number)
   auto fetch = [&](int sl) {
     const int sc = max(sl, 0);
 #pragma unroll
@@ -1305,7 +1309,10 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
     if (mask != ~0u)
 #pragma unroll
       for (int j = 0; j < RI; ++j)
-        if (!((mask >> (j * RPI + lane / NCH)) & 1)) vr[j] = u32x4_t{0, 0, 0, 0};
+        if (!((mask >> (j * RPI + lane / NCH)) & 1)) {
+          vr[j] = u32x4_t{0, 0, 0, 0};
+          if constexpr (FP8) vsc[j] = kScaleOne;
+        }
     put(vr, vsc, fv);      // over K: a wave's LDS accesses keep their order
     if (i + 1 < nblk) {
       const int sl = slots_of(i + 1, page);
