@@ -22,6 +22,7 @@
 #include <algorithm>
 
 #include "paged.h"
+#include "paged_cut.h"
 
 namespace adept {
 namespace {
@@ -361,11 +362,6 @@ __device__ __forceinline__ int tile_limits(const Entries& e, const PagedView& c,
   const int a = __shfl(lim[0], j & 63, 64), b = __shfl(lim[1], j & 63, 64);
   return j >= tile.cols ? 0 : j < 64 ? a : b;
 }
-__device__ __forceinline__ void part_keys(int n, int parts, int p, int* t0, int* t1) {
-  const int per = ((n + KB - 1) / KB + parts - 1) / parts * KB;
-  *t0 = min(p * per, n);
-  *t1 = min(*t0 + per, n);
-}
 
 // One workgroup per (tile, K/V head, part of the keys).  Wave w holds columns
 // 32 w .. 32 w + 31.  Scores come transposed, S^T = K Q^T (32 keys x 32 columns,
@@ -434,9 +430,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
     const int32_t* pages = c.table + (int64_t)tile.seq * c.max_pages;
     const int j = wave * 32 + c32;
     const bool valid = j < tile.cols;
-    int tend, tb, te;
+    int tend;
     const int qlim = tile_limits(e, c, tile, G, hk, j, &tend);
-    part_keys(tend, whole ? 1 : parts, p, &tb, &te);
+    const KeyRange range = part_of_keys(tend, whole ? 1 : parts, p, KB);
+    const int tb = range.begin, te = range.end;
     const int nkb = (te - tb + KB - 1) / KB;
     auto key_of = [&](int kb) { return tb + kb * KB + lane; };
     auto page_of = [&](int kb) { return pages[min(key_of(kb), te - 1) >> c.shift]; };
@@ -890,8 +887,8 @@ __global__ __launch_bounds__(kTile32Threads) void paged_tile_f32_kernel(
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) wend = max(wend, __shfl_xor(wend, o, 64));
     wend = __builtin_amdgcn_readfirstlane(wend);
-    int tb, te;
-    part_keys(tend, whole ? 1 : parts, p, &tb, &te);
+    const KeyRange range = part_of_keys(tend, whole ? 1 : parts, p, KB);
+    const int tb = range.begin, te = range.end;
     const int nkb = (te - tb + KB32 - 1) / KB32;
 
     f32x4_t qf[HD / 16];      // dims 16 i + 4 g + 0 .. 3
