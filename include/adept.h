@@ -405,7 +405,8 @@ adept_status adept_paged_load(adept_dtype dt, const adept_paged_kv* kv, const in
  *  table, n_seq of them), not a whole table.  At most about 2^23 (entry, K/V head)
  *  pairs, else ADEPT_E_INVALID.
  *  workspace: adept_paged_attend_workspace_bytes() bytes, 16-byte aligned; its
- *  contents on entry do not matter.  Calls that may overlap need their own. */
+ *  contents on entry do not matter.  What is made for max_active serves every
+ *  smaller bound.  Calls that may overlap need their own. */
 size_t adept_paged_attend_workspace_bytes(const adept_paged_kv* kv, int n_heads, int max_active,
                                           int n_seq, int max_pages);
 adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv* kv, int n_heads, float scale,

@@ -1081,15 +1081,18 @@ TileShape tile_shape(adept_dtype dt, const adept_paged_kv& kv, int n_heads, int 
   t.cap_tiles = (int)(full + max_active);
   const int64_t base = (int64_t)t.max_tiles * kv.n_kv_heads;
   const bool f32 = dt == ADEPT_F32;
-  t.parts = (int)std::max<int64_t>(
-      1, std::min<int64_t>({(f32 ? kParts32 : kParts) / std::max<int64_t>(base, 1),
-                            ceil_div(keys, f32 ? kPartKeys32 : kPartKeys), 32}));
+  const int64_t slots = f32 ? kParts32 : kParts;      // workgroups that parts make up to
+  const int64_t most = std::min<int64_t>(ceil_div(keys, f32 ? kPartKeys32 : kPartKeys), 32);
+  t.parts = (int)std::max<int64_t>(1, std::min(slots / std::max<int64_t>(base, 1), most));
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   t.off_tiles = 256;
   t.off_starts = t.off_tiles + up((size_t)t.cap_tiles * sizeof(Tile));
   t.off_part = t.off_starts + up(((size_t)max_active + 1) * sizeof(int32_t));
   t.bytes = t.off_part;
-  if (t.parts > 1) t.bytes += (size_t)base * t.parts * TC_ * (kv.head_dim + 2) * sizeof(float);
+  // Fewer tiles are cut into more parts: space for what any smaller call cuts, so
+  // that a workspace serves every bound of the entries up to the one it was made for.
+  if (most > 1)
+    t.bytes += (size_t)std::min(slots, base * most) * TC_ * (kv.head_dim + 2) * sizeof(float);
   return t;
 }
 
@@ -1485,7 +1488,8 @@ StepShape step_shape(const adept_paged_kv& kv, int n_heads, int max_active, int 
   t.items = (int)std::min<int64_t>((int64_t)max_active + t.want, max_active * most);
   t.off_part = ((size_t)max_active * sizeof(int2) + 255) & ~(size_t)255;
   t.bytes = t.off_part;
-  if (t.cut)
+  // fewer entries have shorter stretches: space also where only a smaller call cuts
+  if (keys > kStepUnit)
     t.bytes += ((size_t)std::min(max_active, kStepEntries) + t.want) * n_heads *
                (kv.head_dim + 4) * sizeof(float);
   t.bytes = std::max<size_t>(t.bytes, 256);

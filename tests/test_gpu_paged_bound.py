@@ -1,0 +1,45 @@
+"""A layer step over a paged cache whose caller lowers max_active from layer to layer."""
+import math
+
+import pytest
+import torch
+
+import adept_inputs as ai
+from paper_2601_03700_amd import binding as B
+from tests.test_gpu_paged_model import LLAMA, Checker
+
+from paper_2601_03700_amd.model import DecoderModel
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("n_seq,T,lower", [(1, 1024, 900), (1, 1024, 250), (2, 200, 130)])
+def test_a_lower_bound_of_the_entries(kv, n_seq, T, lower):
+    """The rows that exit at layer 1 are known to the caller: the later steps' bound is the count
+    that is left, in the workspace made for all."""
+    print(f"paged model, bound {n_seq * T} -> {lower}, {kv}", flush=True)
+    shape = LLAMA
+    w = ai.decoder_weights(shape, seed=3, dtype="bf16", std=0.04)
+    model = DecoderModel(shape, w, dtype="bf16", rope_max_pos=8192)
+    n = n_seq * T
+    cache = model.new_paged_cache(n_seq, n_pages=130, page_size=64, kv_dtype=kv)
+    cache.reserve(T)
+    ids = torch.from_numpy(ai.token_ids(2, shape.vocab, n_seq, T)).to(DEV, torch.int32).view(-1)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV).repeat(n_seq)
+    seq = torch.arange(n_seq, dtype=torch.int32, device=DEV).repeat_interleave(T)
+    gone = torch.randperm(n, generator=torch.Generator().manual_seed(1))[:n - lower]
+    force = torch.zeros(n, dtype=torch.int32)
+    force[gone] = 1
+    st = model.new_state(n, pos, seq, cache.slots(pos, seq), force.to(DEV))
+    B.embed(n, shape.d_model, shape.vocab, ids, model.embed, st.h[0])
+    B.token_init(n, shape.n_layers, shape.d_model, st.active[0], st.counts, st.exit_layer, st.inertia)
+    args = model.layer_args(st, cache, B.exit_cfg(math.inf, shape.n_layers), True)
+    check = Checker(model, cache)
+    for i in range(1, shape.n_layers + 1):
+        args.max_active = n if i == 1 else lower
+        B.layer_step_paged(args, cache.kv, cache.page_table, i, st.cache_slot)
+        check(i, st)
+    assert int((st.exit_layer == 1).sum()) == n - lower
+    assert int(st.counts[shape.n_layers & 1]) == lower
