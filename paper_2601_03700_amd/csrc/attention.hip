@@ -733,6 +733,16 @@ size_t attend_workspace_bytes(int max_active, int n_seq, int n_heads, int head_d
   return std::max(tiles, split_workspace_bytes(max_active, n_heads, head_dim, s_max));
 }
 
+// Fewer entries are cut into more chunks, so a smaller call can need more.  Cut at
+// all are calls of fewer than split_target pairs, into at most target + pairs.
+size_t attend_workspace_bound(int max_active, int n_seq, int n_heads, int head_dim, int s_max) {
+  const int64_t most = (s_max + 255) / 256, target = split_target(head_dim);
+  const int64_t pairs = std::min<int64_t>((int64_t)max_active * n_heads, target + n_heads);
+  const size_t split =
+      most > 1 ? (size_t)std::min(pairs * most, target + pairs) * (head_dim + 2) * sizeof(float) : 0;
+  return std::max(attend_workspace_bytes(max_active, n_seq, n_heads, head_dim, s_max), split);
+}
+
 adept_status attend_dispatch(adept_dtype dt, int n_heads, int head_dim, float scale, int causal,
                              const void* q, const int32_t* rows, const int32_t* n_active,
                              int max_active, const int32_t* pos, const int32_t* seq, int n_seq,

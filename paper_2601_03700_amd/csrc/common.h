@@ -395,6 +395,8 @@ adept_status compact_check(int layer, int n_layers, const uint8_t* exit_flag,
 // attention (csrc/attention.hip): adept_attend with a switch that can forbid
 // the query-tile kernel (one query per sequence: decode)
 size_t attend_workspace_bytes(int max_active, int n_seq, int n_heads, int head_dim, int s_max);
+// enough for every call of at most max_active entries
+size_t attend_workspace_bound(int max_active, int n_seq, int n_heads, int head_dim, int s_max);
 adept_status attend_dispatch(adept_dtype dt, int n_heads, int head_dim, float scale, int causal,
                              const void* q, const int32_t* rows, const int32_t* n_active,
                              int max_active, const int32_t* pos, const int32_t* seq, int n_seq,

@@ -70,7 +70,7 @@ LayerWs carve(const adept_layer_args* a, void* base, const PagedStep* pg) {
   w.compact = p + off; off += align256(w.compact_bytes);
   w.attend_bytes = pg ? adept_paged_attend_workspace_bytes(pg->kv, a->n_heads, a->n_tok, a->n_seq,
                                                            pg->max_pages)
-                      : attend_workspace_bytes(a->n_tok, a->n_seq, a->n_heads, a->head_dim, a->s_max);
+                      : attend_workspace_bound(a->n_tok, a->n_seq, a->n_heads, a->head_dim, a->s_max);
   w.attend = p + off; off += align256(w.attend_bytes);
   const bool gpt2 = a->family == ADEPT_FAMILY_GPT2;
   w.kvgen_bytes = gpt2 ? adept_kv_generate_layernorm_workspace_bytes(a->n_layers, a->n_tok,
