@@ -196,6 +196,8 @@ constexpr float kLazy = 8.0f;   // log2 headroom of the reference max
 // max(a, b, c) in one v_max3_f32.  The scores come from MFMAs, which the
 // compiler cannot prove canonical, so fmaxf would first quiet each input
 // (one extra v_max per value); finite values and -inf need no quieting.
+// The compiler does not see that this reads a product's result and puts no wait
+// for it: some value of each product goes through fmaxf first.
 __device__ __forceinline__ float max3_raw(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
@@ -411,14 +413,13 @@ __global__ __launch_bounds__(kPrefillThreads, 2) void attend_prefill_kernel(
     bool need = false;
 #pragma unroll
     for (int qg = 0; qg < QG; ++qg) {
-      float m = max3_raw(s[qg][0][0], s[qg][0][1], s[qg][0][2]);
-      m = max3_raw(m, s[qg][0][3], s[qg][1][0]);
-      m = max3_raw(m, s[qg][1][1], s[qg][1][2]);
-      m = max3_raw(m, s[qg][1][3], s[qg][2][0]);
-      m = max3_raw(m, s[qg][2][1], s[qg][2][2]);
-      m = max3_raw(m, s[qg][2][3], s[qg][3][0]);
-      m = max3_raw(m, s[qg][3][1], s[qg][3][2]);
-      m = max_column(max3_raw(m, s[qg][3][3], m)) * scale_log2;
+      // one value of each product by fmaxf, which waits for it; the others depend on these
+      float m = fmaxf(fmaxf(s[qg][0][0], s[qg][1][0]), fmaxf(s[qg][2][0], s[qg][3][0]));
+#pragma unroll
+      for (int sb = 0; sb < 4; sb += 2)
+#pragma unroll
+        for (int v = 1; v < 4; ++v) m = max3_raw(m, s[qg][sb][v], s[qg][sb + 1][v]);
+      m = max_column(m) * scale_log2;
       mblk[qg] = m;
       // the reference max moves only when the block exceeds it by more than
       // 2^kLazy: the weights exp2(s - m_ref) then stay below 2^kLazy, and
