@@ -271,15 +271,20 @@ __device__ __forceinline__ bool finite(float x) {
 // LDS address), from an address of each lane or from a uniform one and a byte
 // offset of each lane.  Waited for by wait_loads(): the compiler, where it knows of
 // such a load, puts a wait for all of them in front of every transposing LDS read.
+// m0 is named as overwritten, so that nothing of the compiler's stays in it (it
+// warns that a reserved register keeps no value across the block, as is meant).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds16(const char* src, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void load_lds16(const char* base, uint32_t off, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off),
                "s"(base), "s"(dst)
-               : "memory");
+               : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(
       __attribute__((address_space(3))) const char*)p);
@@ -292,6 +297,14 @@ __device__ __forceinline__ int lane_here() {
   return l;
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Between a wave's LDS writes and its reads of what other lanes wrote (and the
+// other way round): the hardware keeps a wave's LDS accesses in order, this keeps
+// the compiler from changing it.  No instruction.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
 
 // (m, l, o) += the same of other keys; m in the exp2 domain.  Parts without keys
 // have l = 0 and o = 0.
@@ -770,6 +783,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
           *reinterpret_cast<uint2*>(row + ((db * 4 + v / 4) ^ (c32 & (NCO - 1))) * 16 + 8 * hh) =
               make_uint2(pack_bf16x2(o[db][v] * inv, o[db][v + 1] * inv),
                          pack_bf16x2(o[db][v + 2] * inv, o[db][v + 3] * inv));
+      wave_lds_order();
 #pragma unroll
       for (int i = 0; i < 32 * NCO / 64; ++i) {
         const int r = i * (64 / NCO) + lane / NCO, ch = lane % NCO;
@@ -1294,6 +1308,7 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
       }
     };
     put(kr, ksc, fk);
+    wave_lds_order();
     f32x4_t s[2];
 #pragma unroll
     for (int sb = 0; sb < 2; ++sb) {
@@ -1313,7 +1328,9 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
           vr[j] = u32x4_t{0, 0, 0, 0};
           if constexpr (FP8) vsc[j] = kScaleOne;
         }
-    put(vr, vsc, fv);      // over K: a wave's LDS accesses keep their order
+    wave_lds_order();
+    put(vr, vsc, fv);      // over K
+    wave_lds_order();
     if (i + 1 < nblk) {
       const int sl = slots_of(i + 1, page);
       there = (uint32_t)__ballot(sl >= 0);
@@ -1366,6 +1383,7 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
           bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
       o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb, o[db], 0, 0, 0);
     }
+    wave_lds_order();      // the next block's K, or the results, lie over V
   }
 
   // the four waves' results
