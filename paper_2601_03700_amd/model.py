@@ -116,11 +116,11 @@ class PagedKVCache:
 
     def slots(self, pos, seq):
         """Slots (int32) of tokens at pos of sequences seq, both int32 device tensors; the last
-        slot of the cache where a sequence has no page."""
-        p = pos.long()
+        slot of the cache where a sequence has no page, or is none of the cache's."""
+        p, b = pos.long(), seq.long()
         at = (p // self.page_size).clamp(0, self.max_pages - 1)
-        page = self.page_table[seq.long(), at]
-        there = (page >= 0) & (p >= 0) & (p < self.s_max)
+        page = self.page_table[b.clamp(0, self.n_seq - 1), at]
+        there = (page >= 0) & (p >= 0) & (p < self.s_max) & (b >= 0) & (b < self.n_seq)
         return torch.where(there, page * self.page_size + (p % self.page_size).to(torch.int32),
                            self.n_slots - 1).to(torch.int32)
 
