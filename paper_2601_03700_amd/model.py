@@ -89,11 +89,17 @@ class PagedKVCache:
         scales = (None, None) if self.k_scale is None else (self.k_scale[i], self.v_scale[i])
         return B.paged_kv(self.k[i], self.v[i], self.page_size, *scales)
 
+    def _check_sequence(self, seq):
+        if not 0 <= seq < self.n_seq:
+            raise ValueError(f"sequence {seq}: the cache has {self.n_seq}")
+
     def reserve(self, lengths):
         """Pages for lengths[b] tokens of sequence b (a dict or one number for all); raises
         ValueError, with nothing taken, where they do not fit."""
         if not isinstance(lengths, dict):
             lengths = {b: int(lengths) for b in range(self.n_seq)}
+        for b in lengths:
+            self._check_sequence(b)
         more = {b: -(-n // self.page_size) - len(self._pages[b]) for b, n in lengths.items()}
         for b, n in lengths.items():
             if not 0 <= n <= self.s_max:
@@ -110,6 +116,7 @@ class PagedKVCache:
 
     def release(self, seq):
         """Gives the sequence's pages back (its tokens are gone)."""
+        self._check_sequence(seq)
         self._free += reversed(self._pages[seq])
         self._pages[seq] = []
         self.page_table[seq].fill_(-1)
