@@ -378,6 +378,11 @@ class DecoderModel:
         if pmax >= self.rope_max_pos or pmax >= s_max:
             raise ValueError(f"position {pmax} outside rotary table / cache")
 
+    @staticmethod
+    def _check_sequences(cache, n):
+        if n > cache.n_seq:
+            raise ValueError(f"{n} sequences, the cache has {cache.n_seq}")
+
     def token_pass(self, ids, pos, seq, cache, cfg, force_layer=None, attn_tiles=True,
                    logit_rows=None, on_layer=None):
         """Run token rows (ids/pos/seq: int32 device tensors [n]) through all layers.  Over a
@@ -425,20 +430,16 @@ class DecoderModel:
         a prompt can be run in pieces."""
         ids = torch.as_tensor(np.asarray(ids) if not isinstance(ids, torch.Tensor) else ids)
         Bn, T = ids.shape
-        s_max = T if s_max is None else s_max
         dev = self.device
         if start < 0 or (start > 0 and cache is None):
             raise ValueError(f"a prompt from position {start} on continues a cache")
         if cache is None:
-            cache = self.new_cache(Bn, s_max)
-        elif start or isinstance(cache, PagedKVCache):
-            s_max = cache.s_max
+            cache = self.new_cache(Bn, T if s_max is None else s_max)
+        self._check_sequences(cache, Bn)
         pos = torch.arange(start, start + T, dtype=torch.int32, device=dev).repeat(Bn)
         seq = torch.arange(Bn, dtype=torch.int32, device=dev).repeat_interleave(T)
-        self._check_positions(pos, s_max, pos_max=start + T - 1)
+        self._check_positions(pos, cache.s_max, pos_max=start + T - 1)
         if isinstance(cache, PagedKVCache):
-            if Bn > cache.n_seq:
-                raise ValueError(f"{Bn} sequences, the cache has {cache.n_seq}")
             cache.reserve({b: start + T for b in range(Bn)})
         fl = None
         if isinstance(force_layer, torch.Tensor):
@@ -461,10 +462,9 @@ class DecoderModel:
         dev = self.device
         n = int(ids.shape[0])
         seq = torch.arange(n, dtype=torch.int32, device=dev)
+        self._check_sequences(cache, n)
         self._check_positions(pos, cache.s_max, pos_max)
         if isinstance(cache, PagedKVCache):
-            if n > cache.n_seq:
-                raise ValueError(f"{n} sequences, the cache has {cache.n_seq}")
             at = [pos_max] * n if pos_max is not None else pos.tolist()
             cache.reserve({b: int(p) + 1 for b, p in enumerate(at)})
         rows = torch.arange(n, dtype=torch.int32, device=dev)

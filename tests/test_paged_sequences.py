@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2601_03700_amd.model import PagedKVCache
+from paper_2601_03700_amd.model import DecoderModel, KVCache, PagedKVCache
 
 
 def cache(n_seq=3, n_pages=9, page=4, max_pages=3, kv="bf16"):
@@ -31,3 +31,44 @@ def test_sequences_outside_the_cache_have_no_pages(seq):
     with pytest.raises(ValueError, match="sequence"):
         c.release(seq)
     assert torch.equal(c.page_table, table) and c.free_pages == free
+
+
+class Reached(Exception):
+    pass
+
+
+class HostModel(DecoderModel):
+    """The checks before a pass, without the pass."""
+
+    def __init__(self):
+        self.device, self.rope_max_pos = torch.device("cpu"), 64
+
+    def token_pass(self, *args):
+        raise Reached
+
+
+def flat(n_seq=2, s_max=8):
+    k = torch.zeros((1, n_seq * s_max, 2, 16))
+    return KVCache(k, k.clone(), n_seq, s_max)
+
+
+@pytest.mark.parametrize("make", [flat, lambda: cache(n_seq=2, n_pages=4, page=4, max_pages=2)])
+def test_passes_that_a_given_cache_cannot_hold(make):
+    """More sequences or tokens than the cache has slots for would be written behind it."""
+    m = HostModel()
+    ids = lambda b, t: torch.zeros((b, t), dtype=torch.int32)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32)
+    for fits in (dict(ids=ids(2, 8)), dict(ids=ids(1, 3), start=5)):
+        with pytest.raises(Reached):
+            m.prefill(cfg=None, cache=make(), **fits)
+    for bad in (dict(ids=ids(3, 4)), dict(ids=ids(3, 4), start=2), dict(ids=ids(2, 9)),
+                dict(ids=ids(2, 9), s_max=9), dict(ids=ids(1, 4), start=5)):
+        with pytest.raises(ValueError):
+            m.prefill(cfg=None, cache=make(), **bad)
+    with pytest.raises(Reached):
+        m.decode_step(make(), i32(1, 1), i32(7, 0), None)
+    for n, pos in ((3, i32(1, 1, 1)), (2, i32(8, 0))):
+        with pytest.raises(ValueError):
+            m.decode_step(make(), i32(*[1] * n), pos, None)
+        with pytest.raises(ValueError):
+            m.decode_step(make(), i32(*[1] * n), pos, None, pos_max=int(pos.max()))
