@@ -432,7 +432,7 @@ def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
               "paged_kv", "scales must be contiguous uint8 [n_slots, Hkv]")
     kv = PagedKv(_KV_TYPES[k.dtype], k.shape[1], k.shape[2], page_size, k.shape[0] // page_size,
                  ptr(k), ptr(v), ptr(k_scale), ptr(v_scale))
-    kv.tensors = (k, v, k_scale, v_scale)
+    kv.tensors, kv.layers = (k, v, k_scale, v_scale), None
     return kv
 
 
@@ -530,6 +530,14 @@ def layer_paged_workspace_bytes(args: LayerArgs, kv, max_pages):
     return lib().adept_layer_paged_workspace_bytes(ctypes.byref(args), ctypes.byref(kv), max_pages)
 
 
+def _layers_from(kv):
+    """Layers of a cache from the described one on, by the memory behind its tensors."""
+    if kv.layers is None:
+        kv.layers = min((t.untyped_storage().nbytes() - t.storage_offset() * t.element_size()) //
+                        max(t.numel() * t.element_size(), 1) for t in kv.tensors if t is not None)
+    return kv.layers
+
+
 def layer_step_paged(args: LayerArgs, kv, page_table, layer, cache_slot=None, stream=None):
     """layer_step over a paged cache; kv: paged_kv of its first layer, the others behind it;
     page_table int32 [n_seq, max_pages]; cache_slot int32, one for each row (8-bit caches)."""
@@ -537,6 +545,9 @@ def layer_step_paged(args: LayerArgs, kv, page_table, layer, cache_slot=None, st
         raise AdeptError("layer_step_paged: page_table must be [n_seq, max_pages]")
     if cache_slot is not None and cache_slot.numel() < args.n_tok:
         raise AdeptError("layer_step_paged: one slot for each row")
+    if _layers_from(kv) < args.n_layers:
+        raise AdeptError(f"layer_step_paged: {args.n_layers} layers, the cache has "
+                         f"{kv.layers} from the described one on")
     dev = _device_of("layer_step_paged", kv)
     tp, cp = _i32_ptrs("layer_step_paged", dev, page_table, cache_slot)
     _check(lib().adept_layer_step_paged(ctypes.byref(args), ctypes.byref(kv), tp,
