@@ -493,8 +493,8 @@ def paged_attend(kv, q, rows, n_active, max_active, pos, seq, n_seq, page_table,
     """Attention of the entries q [max_active, H, hd] over the paged cache kv; page_table int32
     [n_seq, max_pages].  workspace: uint8, paged_attend_workspace_bytes()."""
     dev = _device_of("paged_attend", kv)
-    n, H, hd = q.shape
-    if not (q.is_contiguous() and out.is_contiguous() and out.dtype is q.dtype and
+    n, H, hd = q.shape if q.dim() == 3 else (-1, 0, 0)
+    if not (n >= 0 and q.is_contiguous() and out.is_contiguous() and out.dtype is q.dtype and
             hd == kv.head_dim and n >= max_active and out.numel() >= max_active * H * hd and
             rows.numel() >= max_active and
             (q.dtype is torch.bfloat16 or q.dtype is torch.float32)):
