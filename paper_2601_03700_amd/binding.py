@@ -413,6 +413,12 @@ def _device_of(what, kv):
     return dev
 
 
+def _count(what, n_rows):
+    """A count is one number; an empty tensor's address would be that of no count."""
+    if n_rows is not None and n_rows.numel() != 1:
+        raise AdeptError(f"{what}: n_rows must hold one number")
+
+
 def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
     """Descriptor of one layer's paged cache: k, v [n_slots, Hkv, hd] (f32, bf16, or e4m3 codes as
     uint8 / float8_e4m3fn with k_scale, v_scale uint8 [n_slots, Hkv]), contiguous, n_slots a
@@ -458,6 +464,7 @@ def paged_store(kv, k, v, slot, rows=None, n_rows=None, stream=None):
     if it is an 8-bit one; rows: the listed rows only, n_rows (device int32 [1]): how many of
     them."""
     dev = _device_of("paged_store", kv)
+    _count("paged_store", n_rows)
     kp, ks = _rows("paged_store", kv, dev, k, k.dtype)
     vp, vs = _rows("paged_store", kv, dev, v, k.dtype)
     sp, rp, np_ = _i32_ptrs("paged_store", dev, slot, rows, n_rows)
@@ -473,6 +480,7 @@ def paged_store(kv, k, v, slot, rows=None, n_rows=None, stream=None):
 def paged_load(kv, slot, k, v, n_rows=None, stream=None):
     """k[i], v[i] = the cache's values at slot[i] (k, v [n, Hkv, hd], any row stride)."""
     dev = _device_of("paged_load", kv)
+    _count("paged_load", n_rows)
     kp, ks = _rows("paged_load", kv, dev, k, k.dtype)
     vp, vs = _rows("paged_load", kv, dev, v, k.dtype)
     sp, np_ = _i32_ptrs("paged_load", dev, slot, n_rows)

@@ -23,3 +23,13 @@ def on_the_current_device(monkeypatch):
 def test_queries_that_have_no_heads(dims):
     with pytest.raises(B.AdeptError, match="q and out"):
         B.paged_attend(KV, t(*dims), I32, I32, 4, I32, I32, 1, I32.view(1, 4), t(*dims))
+
+
+@pytest.mark.parametrize("call", [
+    lambda n: B.paged_store(KV, t(4, 2, 64), t(4, 2, 64), I32, n_rows=n),
+    lambda n: B.paged_store(KV, t(4, 2, 64), t(4, 2, 64), I32, rows=I32, n_rows=n),
+    lambda n: B.paged_load(KV, I32, t(4, 2, 64), t(4, 2, 64), n_rows=n)])
+def test_a_count_of_no_elements(call):
+    """Its address is NULL, which would stand for all rows."""
+    with pytest.raises(B.AdeptError, match="n_rows"):
+        call(I32[:0])
