@@ -414,9 +414,9 @@ def _device_of(what, kv):
 
 
 def _count(what, n_rows):
-    """A count is one number; an empty tensor's address would be that of no count."""
-    if n_rows is not None and n_rows.numel() != 1:
-        raise AdeptError(f"{what}: n_rows must hold one number")
+    """A count is the first number; an empty tensor's address would be that of no count."""
+    if n_rows is not None and n_rows.numel() == 0:
+        raise AdeptError(f"{what}: n_rows holds no number")
 
 
 def paged_kv(k, v, page_size, k_scale=None, v_scale=None):
