@@ -1359,16 +1359,23 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
         for (int v = 0; v < 4; ++v) o[d][v] *= alpha;
     }
     const float msub = m_ref == -INFINITY ? 0.0f : m_ref;
-    constexpr bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
-    uint32_t w[4];
+    // A weight is the sum of two bf16 values, 16 bits of it, and the normaliser takes it
+    // whole: the products wait for the keys, so a second one costs nothing (64 x 4096
+    // 654 us with one and with two, in 8 bits 355 and 353; against 64 bits 0.0016 of the
+    // result, its own rounding, and 0.0017).
+    uint32_t hi[4], lo[4];
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
       const float a = s[y >> 1][2 * (y & 1)], b = s[y >> 1][2 * (y & 1) + 1];
-      w[y] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(a, scale_log2, -msub)),
-                         __builtin_amdgcn_exp2f(fmaf(b, scale_log2, -msub)));
-      l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[y]), ones, l_run, false);
+      const float pa = __builtin_amdgcn_exp2f(fmaf(a, scale_log2, -msub));
+      const float pb = __builtin_amdgcn_exp2f(fmaf(b, scale_log2, -msub));
+      hi[y] = pack_bf16x2(pa, pb);
+      lo[y] = pack_bf16x2(pa - __uint_as_float(hi[y] << 16),
+                          pb - __uint_as_float(hi[y] & 0xffff0000u));
+      l_run += pa + pb;
     }
-    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+    const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+    const bf16x8_t pl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       s16x4 half[2];
@@ -1381,7 +1388,8 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
       }
       const bf16x8_t a = __builtin_bit_cast(
           bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
-      o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb, o[db], 0, 0, 0);
+      o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ph, o[db], 0, 0, 0);
+      o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pl, o[db], 0, 0, 0);
     }
     wave_lds_order();      // the next block's K, or the results, lie over V
   }
