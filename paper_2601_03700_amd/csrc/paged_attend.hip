@@ -1158,11 +1158,11 @@ __device__ __forceinline__ Stretch step_stretch(const Entries& e, const PagedVie
   if (tid < 6) s_out[tid] = 0;
   __syncthreads();
   sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-  const int cut = (int)max((sum + want - 1) / want, (long long)least);   // units of a stretch
+  const int cut = stretch_units(sum, want, least);
   int cnt = 0;
 #pragma unroll
   for (int i = 0; i < P; ++i)
-    cnt += tid * P + i < n ? max((units[i] + cut - 1) / cut, 1) : 0;
+    cnt += tid * P + i < n ? stretches(units[i], cut) : 0;
   int scan = cnt;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -1175,7 +1175,7 @@ __device__ __forceinline__ Stretch step_stretch(const Entries& e, const PagedVie
   for (int w = 0; w < wave; ++w) at += s_cnt[w];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const int parts = tid * P + i < n ? max((units[i] + cut - 1) / cut, 1) : 0;
+    const int parts = tid * P + i < n ? stretches(units[i], cut) : 0;
     if (x >= at && x < at + parts) {
       s_out[0] = tid * P + i;
       s_out[1] = x - at;

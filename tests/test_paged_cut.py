@@ -14,24 +14,28 @@ SIZES = sorted({n for k in (0, 1, 31, 63, 64, 65, 127, 128, 1000, 16384, 40000, 
                 if 0 <= n <= MOST} | {512 * 4194301})
 
 
-@pytest.fixture(scope="module")
-def cuts(tmp_path_factory):
-    """{(n, parts): [(begin, end), ...]}"""
-    d = tmp_path_factory.mktemp("cut")
-    asked = [(n, parts) for n in SIZES for parts in range(1, 33)]
-    src = ["#include <cstdio>", '#include "paged_cut.h"', "int main() { int n, parts;",
-           'while (std::scanf("%d %d", &n, &parts) == 2) for (int p = 0; p < parts; ++p) {',
-           f"const adept::KeyRange r = adept::part_of_keys(n, parts, p, {BLOCK});",
-           'std::printf("%d %d\\n", r.begin, r.end); } }']
+def host(d, lines, asked):
+    """Output lines of a program that includes the header, for lines of input."""
+    src = ["#include <cstdio>", '#include "paged_cut.h"', "int main() {", *lines, "}"]
     (d / "cut.cpp").write_text("\n".join(src))
     # an overflow of int ends the program
     subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all",
                     "-I", CSRC, "-o", str(d / "cut"), str(d / "cut.cpp")], check=True)
-    r = subprocess.run([str(d / "cut")], input="\n".join(f"{n} {p}" for n, p in asked),
+    r = subprocess.run([str(d / "cut")], input="\n".join(" ".join(map(str, a)) for a in asked),
                        capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
-    out = iter(r.stdout.split("\n"))
-    return {key: [tuple(map(int, next(out).split())) for _ in range(key[1])] for key in asked}
+    return [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
+
+
+@pytest.fixture(scope="module")
+def cuts(tmp_path_factory):
+    """{(n, parts): [(begin, end), ...]}"""
+    asked = [(n, parts) for n in SIZES for parts in range(1, 33)]
+    out = iter(host(tmp_path_factory.mktemp("cut"), [
+        'int n, parts; while (std::scanf("%d %d", &n, &parts) == 2) for (int p = 0; p < parts; ++p) {',
+        f"const adept::KeyRange r = adept::part_of_keys(n, parts, p, {BLOCK});",
+        'std::printf("%d %d\\n", r.begin, r.end); }'], asked))
+    return {key: [next(out) for _ in range(key[1])] for key in asked}
 
 
 @pytest.mark.parametrize("n", SIZES)
@@ -45,3 +49,23 @@ def test_parts_take_each_key_once(cuts, n):
         assert at == n
         # a part looks up to two blocks past its end
         assert max(e for _, e in cuts[n, parts]) + 3 * BLOCK < 2 ** 31
+
+
+@pytest.mark.parametrize("entries", [1, 2, 40, 1023, 1024])
+def test_stretches_of_single_entries(tmp_path, entries):
+    """Entries of up to the most tokens, and as few stretches wanted as one: each unit is taken
+    once, by at most wanted + entries stretches."""
+    unit = 128
+    most = -(-MOST // unit)
+    asked = [(u * entries, want, least, u) for u in (0, 1, 2, 31, 1000, 2 ** 18, most - 1, most)
+             for want in (1, 2, 3, 64, 2048) for least in (1, 2, 4)]
+    out = host(tmp_path, [
+        'long long sum; int want, least, units;',
+        'while (std::scanf("%lld %d %d %d", &sum, &want, &least, &units) == 4) {',
+        "const int cut = adept::stretch_units(sum, want, least);",
+        'std::printf("%d %d\\n", cut, adept::stretches(units, cut)); }'], asked)
+    assert len(out) == len(asked)
+    for (_, want, least, units), (cut, parts) in zip(asked, out):
+        assert cut >= least and parts >= 1
+        assert (parts - 1) * cut < max(units, 1) <= max(parts * cut, 1)
+        assert parts * entries <= want + entries
