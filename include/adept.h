@@ -396,8 +396,11 @@ adept_status adept_paged_load(adept_dtype dt, const adept_paged_kv* kv, const in
  *  key_live [n_pages*page_size] uint8, by slot, nullable: slots with 0 are
  *  left out.
  *  out [max_active][H][hd] (dt): softmax(q K^T * scale) V per head, scores and
- *  sums in f32; zeros for an entry that sees no key (or whose sequence is
- *  outside 0 .. n_seq-1).  What is left out has no influence, whatever it holds.
+ *  sums in f32; zeros for an entry that sees no key, or none with a score above
+ *  minus infinity (or whose sequence is outside 0 .. n_seq-1).  What is left out
+ *  has no influence, whatever it holds.  The weights that meet V keep 16 bits for
+ *  one bf16 entry per sequence; in the tiles of bf16 entries they are rounded to
+ *  bf16, in the normaliser as well; in all other cases they are f32.
  *  Entries behind the last active one are left as they were.
  *  Where max_active <= n_seq every entry reads its keys for itself (one new token
  *  per sequence); else the entries of a sequence share them in tiles.  So a call
