@@ -388,13 +388,18 @@ __device__ __forceinline__ int tile_limits(const Entries& e, const PagedView& c,
 // matrix instruction runs 32 cycles and takes 4 to issue), then these are
 // multiplied into the output.  So K of block kb + 1 is needed before V of block kb
 // is done with: two stages of K, three of V, one barrier a block, block kb + 2 on
-// its way while block kb + 1 is computed.  Bound by the SIMDs' instruction issue:
-// a 64-key block of a wave takes some 1900 cycles of its SIMD, 1024 of them matrix
-// instructions, the exponentials 512 and the rest of the softmax about 450.  8
-// prompts of 2048 tokens, 32 heads of 128: 370 us with the plan (0.74 PFLOP/s);
-// 500 tokens over 7900 in 8 bits, 64/8 heads: 161 us with the join (0.83).  Waves
-// of 64 columns, which read each fragment for two products but leave a SIMD one
-// wave: 503 us for the 8 prompts.
+// its way while block kb + 1 is computed.  Bound by neither unit alone: a 64-key block
+// of a wave takes some 2400 cycles of its SIMD (counters: 500 tokens over 7900 in 8
+// bits 2380, 8 prompts of 2048 in bf16 2500), 1024 of them matrix instructions.  A
+// wave issues 2100 cycles a block itself (vector units 1200, the exponentials among
+// them, LDS 220 .. 380, scalar 360 .. 520), which the other wave of the SIMD only partly
+// overlaps: it waits for an issue slot 28 % of its time, for LDS, loads and the barrier
+// about as long; and no wave is there for 8 .. 15 % of the time, before and behind the
+// workgroups.  37 % of the matrix cores' cycles in all.  8 prompts of 2048 tokens, 32
+// heads of 128: 365 us with the plan (0.75 PFLOP/s); 500 tokens over 7900 in 8 bits,
+// 64/8 heads: 163 us with the join (0.82).  Waves of 64 columns, which read each
+// fragment for two products but leave a SIMD one wave: 503 us for the 8 prompts.  The
+// kernels for 128 dims spill 2 and 28 registers (8 bits), outside the loop over keys.
 //
 // A bf16 cache is copied to LDS by direct loads; an 8-bit one goes through
 // registers, where its codes become bf16 with their scale in the conversion itself
@@ -628,11 +633,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(
     // One step of the pipeline: the scores `sn` of the next 32 keys (K at ka) beside
     // the weights of these 32 (scores sc), two exponentials to a product; then these
     // into the output (V at va) beside the maximum of sn, which is returned.  The
-    // weights are rounded to bf16 (the sum takes the rounded ones, as the product
-    // does).  run: loads on the way, one pair to a product.  Of the two waves of a
-    // SIMD the one in a step goes first where the other one converts codes or sets
-    // out (1 x 500 over 8 bits 161 us, 167 without; 5 x 250 heads of 64 22.8, 23.6;
-    // bf16 of 128, whose waves do little else, 370 either way).
+    // weights are rounded to bf16 for the product, as adept_attend's are (the sum takes
+    // the rounded ones, so that they still add up to one): at most 2^-8 of a weight,
+    // 0.0019 of the result against 64 bits where its own rounding alone makes 0.0016.
+    // Weights of 16 bits, by a second product for what the first leaves, were measured:
+    // 0.0016, for 495 us instead of 364 (8 x 2048), 212 instead of 163 (1 x 500).
+    // run: loads on the way, one pair to a product.  Of the two waves of a SIMD the
+    // one in a step goes first where the other one converts codes or sets out (1 x
+    // 500 over 8 bits 161 us, 167 without; 5 x 250 heads of 64 22.8, 23.6; bf16 of
+    // 128, whose waves do little else, 370 either way).
     auto step = [&](bool run, uint32_t ka, f32x16_t& sn, uint32_t va, const f32x16_t& sc,
                     uint32_t ko, uint32_t vo) {
       constexpr int AHEAD = 3, EPS = 16 / DS;    // fragments read ahead, weights of a product

@@ -52,7 +52,9 @@ class PagedKVCache:
     page_table [n_seq, max_pages] int32 on the device (-1: no page); which pages are free is
     known on the host.  One page more, which no table names, takes the K/V of tokens that have
     no place.  A pass over an "fp8" cache holds its own rows' K and V of all layers in the
-    model's type beside it: long prompts are better run in pieces (prefill with start)."""
+    model's type beside it: long prompts are better run in pieces (prefill with start).  Its
+    decode passes need the K/V generation inside the layers (kv_fused, bf16 models); without
+    it they run as prompts do, their attention in tiles: right, and slower."""
 
     def __init__(self, n_layers, n_heads, head_dim, n_seq, n_pages, page_size, max_pages, kv_dtype,
                  device):
