@@ -1257,6 +1257,12 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
   f32x4_t o[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  // of the weights' second parts, where V can be infinite (no e4m3 value is): their
+  // product with it may be NaN or the other infinity, and must not meet the first's
+  constexpr int DB2 = FP8 ? 1 : DB;
+  f32x4_t o2[DB2];
+#pragma unroll
+  for (int i = 0; i < DB2; ++i) o2[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m_ref = -INFINITY, l_run = 0.0f;
 
   const int nblk = (st.t1 - st.t0 + kStepUnit - 1) / kStepUnit;   // blocks of each wave
@@ -1365,7 +1371,10 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) o[d][v] *= alpha;
+        for (int v = 0; v < 4; ++v) {
+          o[d][v] *= alpha;
+          if constexpr (!FP8) o2[d][v] *= alpha;
+        }
     }
     const float msub = m_ref == -INFINITY ? 0.0f : m_ref;
     // A weight is the sum of two bf16 values, 16 bits of it, and the normaliser takes it
@@ -1398,10 +1407,17 @@ __global__ __launch_bounds__(256, FP8 || HD == 64 ? 3 : 2) void paged_step_kerne
       const bf16x8_t a = __builtin_bit_cast(
           bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
       o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ph, o[db], 0, 0, 0);
-      o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pl, o[db], 0, 0, 0);
+      f32x4_t& second = FP8 ? o[db] : o2[FP8 ? 0 : db];
+      second = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pl, second, 0, 0, 0);
     }
     wave_lds_order();      // the next block's K, or the results, lie over V
   }
+
+  if constexpr (!FP8)
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[d][v] += finite(o2[d][v]) ? o2[d][v] : 0.0f;
 
   // the four waves' results
   float l = l_run;

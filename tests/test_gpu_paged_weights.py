@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from tests import paged_ref as R
 from tests.test_gpu_paged_attend import Case
 
 pytestmark = pytest.mark.gpu
@@ -29,3 +30,24 @@ def test_only_the_result_is_rounded_to_bf16(cache, H, heads, hd, shape):
     worst = ((out.double() - ref).abs() / tol).max().item()
     print(f"  worst error / bound {worst:.3f}", flush=True)
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("H,heads,hd", [(4, 4, 64), (8, 2, 128), (2, 1, 32)])
+@pytest.mark.parametrize("context", [0, 40, 200, 3000])
+def test_infinite_values_that_are_seen(H, heads, hd, context):
+    """An infinite V of a seen key: that dim of the result is this infinity, NaN where both signs
+    meet, and the other dims are as the definition; nothing of a weight's second part enters."""
+    print(f"paged attend, infinite V, {H}/{heads}x{hd} context={context}", flush=True)
+    c = Case("bf16", "bf16", H, heads, hd, 16, [(context, 1, 1), (7, 1, 1)], seed=32, q_std=0.3)
+    at = [int(c.table[0, t // 16]) * 16 + t % 16 for t in (0, context // 3, context // 2, context)]
+    for d, signs in enumerate([(1, 1, 1, 1), (-1, 0, 0, 0), (0, 1, 0, 0), (0, 0, 0, -1), (0, -1, -1, 1)]):
+        for slot, sign in zip(at, signs):
+            if sign:
+                c.pool[1][slot, :, 3 * d] = sign * torch.inf
+    out, (ref, wv, qk) = c.run().double(), c.ref()
+    assert torch.equal(out.isnan(), ref.isnan())
+    assert torch.equal(out.isposinf(), ref.isposinf()) and torch.equal(out.isneginf(), ref.isneginf())
+    assert out[0].isposinf().any() and not out[1].isinf().any()
+    fine = torch.isfinite(ref)
+    tol = R.bound(c.dt, ref, wv, qk)
+    assert ((out - ref).abs() <= tol)[fine].all()
