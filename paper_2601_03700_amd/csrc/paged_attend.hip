@@ -4,7 +4,7 @@
 // of one sequence are the columns of a matrix; a plan kernel cuts each sequence's
 // columns into tiles of 128.  A workgroup takes one (tile, K/V head) and, where
 // there are too few of those to fill the card, a part of the keys, which a second
-// kernel joins.  Bound by the matrix cores and the softmax beside them.
+// kernel joins.  Bound by the matrix cores and the waves' issue beside them together.
 //
 // Steps (head_dim 64 / 128, bf16, one entry per sequence): a workgroup takes a
 // stretch of one entry's keys for one K/V head; a second kernel joins the

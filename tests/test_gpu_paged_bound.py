@@ -6,9 +6,8 @@ import torch
 
 import adept_inputs as ai
 from paper_2601_03700_amd import binding as B
-from tests.test_gpu_paged_model import LLAMA, Checker
-
 from paper_2601_03700_amd.model import DecoderModel
+from tests.test_gpu_paged_model import LLAMA, Checker
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
