@@ -419,6 +419,102 @@ adept_status adept_paged_attend(adept_dtype dt, const adept_paged_kv* kv, int n_
                                 int max_pages, const int32_t* key_len, const uint8_t* key_live,
                                 void* out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Copies pages in all layers at once: for i < *n_pages (<= max_pages; NULL: exactly
+ * max_pages), page dst_page[i] of each of the n_layers layers (K, V and, in 8 bits,
+ * their scales) becomes page src_page[i], of which n_tokens[i] (nullable: all)
+ * tokens are copied and the rest of the destination is left as it was.  kv
+ * describes the first of the layers, the others lie behind it:
+ * [n_layers][n_pages*page_size][Hkv][hd].  A page outside the cache is skipped.
+ * The destinations are distinct and none of them is a source (of another entry);
+ * a call copies below 2^24 pieces of 16 KiB. */
+adept_status adept_paged_copy(const adept_paged_kv* kv, int n_layers, const int32_t* src_page,
+                              const int32_t* dst_page, const int32_t* n_tokens,
+                              const int32_t* n_pages, int max_pages, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * adept_verify_drafts -- drafted tokens against the model's probabilities: of each
+ * sequence's drafts x_0 .. x_{g-1} the first ones are kept, and one token
+ * follows them, such that every token is distributed as the model's are.
+ *
+ *  With p_i = softmax(target row i / T), q_i = softmax(draft row i / T): draft i is
+ *  kept iff u_i q_i(x_i) < p_i(x_i) and all before it are; the token behind the
+ *  kept ones comes from the distribution proportional to max(p_i - q_i, 0) where
+ *  draft i was the first one not kept, and from p_g where all g were.  It is the
+ *  first token whose running sum (in ascending order of the tokens) exceeds u_last
+ *  times the whole sum.  Where p_i - q_i leaves nothing, p_i.
+ *
+ *  target [n_seq][max_draft+1][vocab] (dt), rows target_stride elements apart;
+ *  draft [n_seq][max_draft][vocab] (dt), rows draft_stride apart, nullable: then
+ *  q_i is 1 at x_i (drafts without probabilities).  Any alignment, any vocabulary.
+ *  tokens [n_seq][max_draft]: the drafts.  A token outside the vocabulary is not kept.
+ *  n_draft [n_seq], nullable (max_draft): g of each sequence, taken within 0 ..
+ *  max_draft; rows behind those in use are not read.
+ *  temperature [n_seq] float, nullable (1): T; 0 and everything else that is not
+ *  above 0: draft i is kept iff it is the first largest of target row i, and the
+ *  token behind is that of its row; u and draft are not used.
+ *  u [n_seq][max_draft+1] float: random numbers in [0, 1), one for each draft and,
+ *  at max_draft, u_last.
+ *  out_tokens [n_seq][max_draft+1]: the kept drafts, the token behind them, then -1.
+ *  n_kept [n_seq].
+ *
+ *  A logit of minus infinity or NaN has no probability; where a row's largest is
+ *  plus infinity, the infinite ones share it.  A row without any probability keeps
+ *  no draft and gives the token -1.  Probabilities and sums are taken in double.
+ *  max_draft = 0 draws a token from each target row.
+ *  workspace: adept_verify_drafts_workspace_bytes(n_seq, max_draft, vocab) bytes,
+ *  16-byte aligned; its contents on entry do not matter.  Calls that may overlap
+ *  need their own.
+ * ------------------------------------------------------------------------- */
+size_t adept_verify_drafts_workspace_bytes(int n_seq, int max_draft, int vocab);
+adept_status adept_verify_drafts(adept_dtype dt, int n_seq, int max_draft, int vocab,
+                                 const void* target, int64_t target_stride, const void* draft,
+                                 int64_t draft_stride, const int32_t* tokens,
+                                 const int32_t* n_draft, const float* temperature, const float* u,
+                                 int32_t* out_tokens, int32_t* n_kept, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Weights in 4 bits, for passes of few rows, which are bound by the weights' bytes:
+ * OCP e2m1 codes (0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign) with one power of two for
+ * every 32 of a row.  A group is quantised to the least 2^E (-100 <= E <= 100) with
+ * which its largest magnitude is at most 7, every value divided by it, rounded to
+ * the nearest code (ties to the even one) and, above 6, taken as 6 (no further off
+ * than a rounding between 4 and 6).  A group with an infinity or NaN is NaN.
+ * All values are exact in bf16: what adept_quant_unpack gives is the same
+ * matrix for the bf16 GEMMs.
+ *
+ * adept_quant_pack: w [n][k] (dt, rows ldw elements apart, any alignment) into
+ * codes and scales, adept_quant_codes_bytes(n, k) / _scales_bytes(n, k) bytes in
+ * this library's own order (blocks of 16 rows and 128 of k, filled up with zeros),
+ * 16-byte aligned.  Matrices of one shape may be stacked.  adept_quant_unpack: back.
+ *
+ * adept_quant_linear: y[i] = x[row] w^T + bias, row = rows ? rows[i] : i, for i <
+ * *n_rows (<= max_rows; NULL: exactly max_rows), later rows of y left as they were.
+ * x [.][k] bf16, rows x_stride elements apart, 16-byte aligned; k and x_stride
+ * multiples of 8; bias [n] bf16, nullable; y [max_rows][n] out_dt, rows y_stride
+ * apart, any alignment.  Products of bf16 numbers, sums in f32.  The weights are
+ * read once for every 64 rows: for many rows the unpacked matrix is faster.
+ * ------------------------------------------------------------------------- */
+size_t adept_quant_codes_bytes(int n, int k);
+size_t adept_quant_scales_bytes(int n, int k);
+adept_status adept_quant_pack(adept_dtype dt, int n, int k, const void* w, int64_t ldw, void* codes,
+                              void* scales, void* stream);
+adept_status adept_quant_unpack(adept_dtype dt, int n, int k, const void* codes, const void* scales,
+                                void* w, int64_t ldw, void* stream);
+adept_status adept_quant_linear(int n, int k, const void* x, int64_t x_stride, const int32_t* rows,
+                                const int32_t* n_rows, int max_rows, const void* codes,
+                                const void* scales, const void* bias, adept_dtype out_dt, void* y,
+                                int64_t y_stride, void* stream);
+
+/* adept_final_logits (norm_bias NULL) or adept_final_logits_layernorm (else) with
+ * the head [vocab][d_model] in 4 bits; bf16 states, d_model a multiple of 8. */
+adept_status adept_final_logits_quant(int d_model, int vocab, float eps, const void* h0_buf,
+                                      const void* h1_buf, const int32_t* exit_layer,
+                                      const int32_t* rows, const int32_t* n_rows, int max_rows,
+                                      const void* norm_gain, const void* norm_bias,
+                                      const void* codes, const void* scales, void* x_norm,
+                                      float* logits, void* stream);
+
 /* ---------------------------------------------------------------------------
  * Whole-layer orchestration of the generative path (Appendix I):
  * adept_layer_step(layer=i) enqueues, for the rows of active[(i-1)&1]

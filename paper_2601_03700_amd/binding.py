@@ -124,6 +124,18 @@ _SIGS = {
     "adept_paged_attend": (_i32, [_i32, ctypes.POINTER(PagedKv), _i32, ctypes.c_float, _i32, _vp,
                                   _vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp,
                                   _sz, _vp]),
+    "adept_paged_copy": (_i32, [ctypes.POINTER(PagedKv), _i32, _vp, _vp, _vp, _vp, _i32, _vp]),
+    "adept_verify_drafts_workspace_bytes": (_sz, [_i32, _i32, _i32]),
+    "adept_verify_drafts": (_i32, [_i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp,
+                                   _vp, _vp, _vp, _sz, _vp]),
+    "adept_quant_codes_bytes": (_sz, [_i32, _i32]),
+    "adept_quant_scales_bytes": (_sz, [_i32, _i32]),
+    "adept_quant_pack": (_i32, [_i32, _i32, _i32, _vp, _i64, _vp, _vp, _vp]),
+    "adept_quant_unpack": (_i32, [_i32, _i32, _i32, _vp, _vp, _vp, _i64, _vp]),
+    "adept_quant_linear": (_i32, [_i32, _i32, _vp, _i64, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp,
+                                  _i64, _vp]),
+    "adept_final_logits_quant": (_i32, [_i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _vp, _i32,
+                                        _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "adept_layer_workspace_bytes": (_sz, [ctypes.POINTER(LayerArgs)]),
     "adept_layer_step": (_i32, [ctypes.POINTER(LayerArgs), _i32, _vp]),
     "adept_layer_paged_workspace_bytes": (_sz, [ctypes.POINTER(LayerArgs), ctypes.POINTER(PagedKv),
@@ -523,6 +535,161 @@ def paged_attend(kv, q, rows, n_active, max_active, pos, seq, n_seq, page_table,
                                     qp, rp, ap, max_active, pp, sp, n_seq, tp, page_table.shape[1],
                                     np_, lp, op, wp, ws_bytes, stream_handle(stream)),
            "adept_paged_attend")
+
+
+def paged_copy(kv, n_layers, src, dst, n_tokens=None, n_pages=None, stream=None):
+    """Pages src[i] of n_layers layers (kv: paged_kv of the first, the others behind it) copied to
+    pages dst[i], of each the first n_tokens[i] tokens; n_pages (device int32 [1]): how many of
+    them.  The destinations are distinct and none of them is a source."""
+    dev = _device_of("paged_copy", kv)
+    _count("paged_copy", n_pages)
+    sp, dp, tp, np_ = _i32_ptrs("paged_copy", dev, src, dst, n_tokens, n_pages)
+    n = src.numel()
+    if dst.numel() != n or (n_tokens is not None and n_tokens.numel() != n):
+        raise AdeptError("paged_copy: one destination and one number of tokens for each page")
+    if _layers_from(kv) < n_layers:
+        raise AdeptError(f"paged_copy: {n_layers} layers, the cache has {kv.layers} from the "
+                         "described one on")
+    _check(lib().adept_paged_copy(ctypes.byref(kv), n_layers, sp, dp, tp, np_, n,
+                                  stream_handle(stream)), "adept_paged_copy")
+
+
+def verify_drafts_workspace_bytes(n_seq, max_draft, vocab):
+    return lib().adept_verify_drafts_workspace_bytes(n_seq, max_draft, vocab)
+
+
+def _logit_rows(what, t, n, per, vocab):
+    """Row stride of logits [n, per, vocab] whose rows follow each other at one distance."""
+    if t.dim() != 3 or t.shape != (n, per, vocab):
+        raise AdeptError(f"{what}: logits must be [{n}, {per}, {vocab}]")
+    if t.is_contiguous() or t.numel() == 0:
+        return vocab
+    s, r, e = t.stride()
+    r = s if per == 1 else r
+    if (vocab > 1 and e != 1) or (n > 1 and s != per * r):
+        raise AdeptError(f"{what}: the rows of logits must be at one distance from each other")
+    return r
+
+
+def verify_drafts(target, draft, tokens, u, out_tokens, n_kept, n_draft=None, temperature=None,
+                  workspace=None, stream=None):
+    """How many of the drafted tokens [n, g] are kept and the token behind them: out_tokens
+    [n, g+1], n_kept [n] int32.  target [n, g+1, V], draft [n, g, V] or None: logits of one type;
+    u [n, g+1] f32 in [0, 1); n_draft [n] int32, temperature [n] f32.  workspace: uint8,
+    verify_drafts_workspace_bytes()."""
+    what = "verify_drafts"
+    dev = target.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise _elsewhere(what)
+    if target.dim() != 3 or target.shape[1] < 1 or target.dtype not in (torch.float32, torch.bfloat16):
+        raise AdeptError(f"{what}: target must be f32 or bf16 [n, drafts + 1, vocab]")
+    n, rows, V = target.shape
+    ts, ds = _logit_rows(what, target, n, rows, V), V
+    if draft is not None:
+        if draft.dtype is not target.dtype:
+            raise AdeptError(f"{what}: target and draft must be of one type")
+        ds = _logit_rows(what, draft, n, rows - 1, V)
+    for t, shape in ((tokens, (n, rows - 1)), (out_tokens, (n, rows)), (n_kept, (n,)), (u, (n, rows)),
+                     (n_draft, (n,)), (temperature, (n,))):
+        if t is not None and tuple(t.shape) != shape:
+            raise AdeptError(f"{what}: a tensor of {shape} expected, not {tuple(t.shape)}")
+    for t in (u, temperature):
+        if t is not None and not (t.dtype is torch.float32 and t.is_contiguous()):
+            raise AdeptError(f"{what}: u and temperature must be contiguous f32")
+    xp, qp, up, mp, wp = _ptrs(what, dev, target, draft, u, temperature, workspace)
+    tp, op, kp, np_ = _i32_ptrs(what, dev, tokens, out_tokens, n_kept, n_draft)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().adept_verify_drafts(dtype_code(target), n, rows - 1, V, xp, ts, qp, ds, tp, np_, mp,
+                                     up, op, kp, wp, ws_bytes, stream_handle(stream)),
+           "adept_verify_drafts")
+
+
+class QuantWeights:
+    """n_mats matrices [n, k] in 4 bits, in the library's order: codes and scales, uint8
+    [n_mats, bytes]."""
+
+    def __init__(self, n, k, codes, scales):
+        self.n, self.k, self.codes, self.scales = n, k, codes, scales
+
+    @property
+    def n_mats(self):
+        return self.codes.shape[0]
+
+
+def quant_weights(n, k, device, n_mats=1):
+    """Room for n_mats matrices [n, k], which quant_pack fills."""
+    cb, sb = lib().adept_quant_codes_bytes(n, k), lib().adept_quant_scales_bytes(n, k)
+    if cb == 0 or n_mats < 1:
+        raise AdeptError(f"quant_weights: no matrix of {n} x {k}")
+    return QuantWeights(n, k, torch.empty((n_mats, cb), dtype=torch.uint8, device=device),
+                        torch.empty((n_mats, sb), dtype=torch.uint8, device=device))
+
+
+def _matrix(what, qw, w, mat):
+    dev = qw.codes.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise _elsewhere(what)
+    if not 0 <= mat < qw.n_mats:
+        raise AdeptError(f"{what}: matrix {mat} of {qw.n_mats}")
+    if w is None:
+        return dev, qw.codes.data_ptr() + mat * qw.codes.stride(0), \
+            qw.scales.data_ptr() + mat * qw.scales.stride(0), None
+    if (w.shape != (qw.n, qw.k) or w.dtype not in (torch.float32, torch.bfloat16) or
+            (qw.k > 1 and w.stride(1) != 1)):
+        raise AdeptError(f"{what}: the matrix must be f32 or bf16 [{qw.n}, {qw.k}] with contiguous rows")
+    if w.get_device() != dev:
+        raise _elsewhere(what)
+    return dev, qw.codes.data_ptr() + mat * qw.codes.stride(0), \
+        qw.scales.data_ptr() + mat * qw.scales.stride(0), w.stride(0) if qw.n > 1 else qw.k
+
+
+def quant_pack(w, qw, mat=0, stream=None):
+    """w [n, k] (f32 or bf16, any row stride) quantised into matrix `mat` of qw."""
+    _, cp, sp, ld = _matrix("quant_pack", qw, w, mat)
+    _check(lib().adept_quant_pack(dtype_code(w), qw.n, qw.k, ptr(w), ld, cp, sp,
+                                  stream_handle(stream)), "adept_quant_pack")
+
+
+def quant_unpack(qw, w, mat=0, stream=None):
+    """w [n, k] = the values of matrix `mat` of qw."""
+    _, cp, sp, ld = _matrix("quant_unpack", qw, w, mat)
+    _check(lib().adept_quant_unpack(dtype_code(w), qw.n, qw.k, cp, sp, ptr(w), ld,
+                                    stream_handle(stream)), "adept_quant_unpack")
+
+
+def quant_linear(x, qw, y, mat=0, rows=None, n_rows=None, bias=None, stream=None):
+    """y[i] = x[row] w^T + bias with matrix `mat` of qw, row = rows[i] (None: i); n_rows (device
+    int32 [1]): how many.  x bf16 [m, k], y f32 or bf16 [rows, n], any row stride."""
+    what = "quant_linear"
+    dev, cp, sp, _ = _matrix(what, qw, None, mat)
+    _count(what, n_rows)
+    if x.dim() != 2 or x.shape[1] != qw.k or x.dtype is not torch.bfloat16 or x.stride(1) != 1:
+        raise AdeptError(f"{what}: x must be bf16 [m, {qw.k}] with contiguous rows")
+    n = x.shape[0] if rows is None else rows.numel()
+    if (y.dim() != 2 or y.shape[0] < n or y.shape[1] != qw.n or (qw.n > 1 and y.stride(1) != 1) or
+            y.dtype not in (torch.float32, torch.bfloat16)):
+        raise AdeptError(f"{what}: y must be f32 or bf16 [{n}, {qw.n}] with contiguous rows")
+    if bias is not None and not (bias.dtype is torch.bfloat16 and bias.shape == (qw.n,) and
+                                 bias.is_contiguous()):
+        raise AdeptError(f"{what}: bias must be contiguous bf16 [{qw.n}]")
+    xp, yp, bp = _ptrs(what, dev, x, y, bias)
+    rp, np_ = _i32_ptrs(what, dev, rows, n_rows)
+    _check(lib().adept_quant_linear(qw.n, qw.k, xp, x.stride(0) if x.shape[0] > 1 else qw.k, rp, np_,
+                                    n, cp, sp, bp, dtype_code(y), yp,
+                                    y.stride(0) if y.shape[0] > 1 else qw.n, stream_handle(stream)),
+           "adept_quant_linear")
+
+
+def final_logits_quant(d_model, vocab, eps, h0, h1, exit_layer, rows, n_rows, max_rows, norm_gain,
+                       norm_bias, qw, x_norm, logits, stream=None):
+    """final_logits (norm_bias None) or final_logits_layernorm over a head in 4 bits."""
+    _, cp, sp, _ = _matrix("final_logits_quant", qw, None, 0)
+    if (qw.n, qw.k) != (vocab, d_model) or h0.dtype is not torch.bfloat16:
+        raise AdeptError(f"final_logits_quant: a bf16 model and a head of {vocab} x {d_model} expected")
+    _check(lib().adept_final_logits_quant(d_model, vocab, eps, ptr(h0), ptr(h1), ptr(exit_layer),
+                                          ptr(rows), ptr(n_rows), max_rows, ptr(norm_gain),
+                                          ptr(norm_bias), cp, sp, ptr(x_norm), ptr(logits),
+                                          stream_handle(stream)), "adept_final_logits_quant")
 
 
 def layer_workspace_bytes(args: LayerArgs):

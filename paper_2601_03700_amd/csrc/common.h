@@ -274,6 +274,11 @@ enum EpiKind {
   EPI_GELU_TANH = 6,  // C[k][n] = gelu(acc) (tanh approximation), dtype
 };
 
+// A matrix in 4 bits (quant.h), and SWIGLU's second one.
+struct QuantView {
+  const uint8_t *codes, *scales, *codes2, *scales2;
+};
+
 struct GemmArgs {
   int M_max;              // grid bound on rows
   const int32_t* M_dev;   // device row count (nullable: M_max exact)
@@ -324,6 +329,9 @@ struct GemmArgs {
   // nullable
   const struct RowList* list;
   const struct RowExit* exit;
+  // bf16, at most 64 rows: the weights' 4-bit form, read instead of B and B2 (which
+  // hold the same values); codes NULL: none
+  QuantView quant;
 };
 // The GLOBAL-metric exit test (Eq. 7-8) run by a residual epilogue over its
 // result rows m (token rows rows[m]): flags and similarities by m, the

@@ -22,6 +22,7 @@
 // 24 rows, QKV / first MLP 13.5 / 13.0 -> 11.0 / 10.3; width 768, 48 rows, biased
 // QKV 9.4 -> 6.8, in the skinny path's order (SPLIT) 8.0.
 #include "gemm_tile.h"
+#include "quant.h"
 
 namespace adept {
 namespace {
@@ -38,15 +39,48 @@ struct DirPre {
   float sc;
 };
 
+// Four columns from n on of row m, any number of columns, any row stride.
+__device__ __forceinline__ void store_any(const GP& p, int m, int n, const float (&v)[4]) {
+  const int64_t at = (int64_t)m * p.ldc + n;
+  const bool whole = n + 4 <= p.N;
+  if (p.c_f32) {
+    float* o = reinterpret_cast<float*>(p.C) + at;
+    if (whole && ((uintptr_t)o & 15) == 0) {
+      *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+      return;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (n + c < p.N) o[c] = v[c];
+    return;
+  }
+  bf16* o = reinterpret_cast<bf16*>(p.C) + at;
+  if (whole && ((uintptr_t)o & 7) == 0) {
+    *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    return;
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    if (n + c < p.N) o[c] = f2bf(v[c]);
+}
+
 // NB == 1 with a pair epilogue (rotary halves, gate and up): the 16 rows of the
 // block are 8 of the first kind and their 8 partners.
 //
 // SPLIT: the sums in the order of the skinny path (gemm.hip), bit for bit: K in
 // the segments its split sp gives these columns' tile, each one chain from zero,
 // added up in ascending order.  The waves take every eighth segment.
-template <int EPI, int NB, int MB, int W, int U, bool SPLIT>
+//
+// Q4: the weights in 4 bits (quant.h), in pieces of 128 of K: 16 bytes and four scale
+// bytes of a lane are its operands of four products.  v_cvt_scalef32_pk_bf16_fp4 makes
+// two bf16 of a byte, times the scale, exactly.  NB == 4 with a pair epilogue: two
+// blocks of the first kind, then their partners.
+template <int EPI, int NB, int MB, int W, int U, bool SPLIT, bool Q4>
 __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, int row_norm,
-                                                             SkSplit sp) {
+                                                             SkSplit sp, QuantView qv) {
+  static_assert(!(SPLIT && Q4) && (NB <= 2 || Q4), "forms");
+  constexpr int KP = Q4 ? kQuantK : BK, HS = KP / 32;   // of K: a piece, products of one
+  constexpr int HALF = NB == 4 ? 2 : 1;                 // blocks of one kind
   extern __shared__ __attribute__((aligned(16))) char smem[];
   float4* red = reinterpret_cast<float4*>(smem);      // [wave or segment][MB * NB][64]
   __shared__ float ssq[W][MB * 16];
@@ -55,12 +89,12 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, q = lane >> 4;
-  const int KT = p.K / BK;
+  const int KT = Q4 ? (p.K + KP - 1) / KP : p.K / BK;
   const bool rope = EPI == EPI_QKV && p.rope_cos;
   const bool pair = EPI == EPI_SWIGLU || rope;
   // the first kind's first column, rows per kind, and the distance to the
   // second kind (SwiGLU's is in B2)
-  const int per = pair && NB == 1 ? 8 : 16;
+  const int per = pair && NB == 1 ? 8 : 16 * HALF;
   int n0, dn = 16;
   if (rope) {
     dn = p.head_dim >> 1;
@@ -69,12 +103,15 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   } else {
     n0 = blockIdx.x * (EPI == EPI_SWIGLU ? per : 16 * NB);
   }
+  // more than 64 rows (plain stores): 64 of them for each grid row
+  const int m0 = Q4 && EPI == EPI_STORE ? (int)blockIdx.y * kDirectRows : 0;
   // raw list entries: loaded before the row count is known, used below it
   int raw[MB];
 #pragma unroll
   for (int y = 0; y < MB; ++y)
-    raw[y] = !rl.exit_layer && p.a_rows ? p.a_rows[min(16 * y + r16, p.M_max - 1)] : 16 * y + r16;
-  constexpr int XB = EPI == EPI_SWIGLU ? 1 : NB;
+    raw[y] = !rl.exit_layer && p.a_rows ? p.a_rows[min(m0 + 16 * y + r16, p.M_max - 1)]
+                                        : m0 + 16 * y + r16;
+  constexpr int XB = EPI == EPI_SWIGLU ? HALF : NB;
   constexpr int G = (MB * XB + W - 1) / W;            // epilogue groups of a wave
   DirPre pre[G];
   constexpr bool kRows = EPI == EPI_RESID || EPI == EPI_QKV;
@@ -97,41 +134,58 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   const int nseg = SPLIT ? (u0 + KT - 1) / sp.U - w0 + 1 : W;
   auto lo_of = [&](int s) { return max((w0 + s) * sp.U - u0, 0); };
   auto hi_of = [&](int s) { return min((w0 + s + 1) * sp.U - u0, KT); };
-  const bf16* br[NB];
-  {
-    const bool two = NB == 1 && pair && r16 >= 8;   // a lane of the second kind
-    const int r = two ? r16 - 8 : r16;
-    br[0] = (EPI == EPI_SWIGLU && two ? p.B2 + (int64_t)(n0 + r) * p.ldb
-                                      : p.B + (int64_t)(n0 + r + (two ? dn : 0)) * p.ldb) + 8 * q;
-    if constexpr (NB == 2)
-      br[1] = (EPI == EPI_SWIGLU ? p.B2 + (int64_t)(n0 + r16) * p.ldb
-                                 : p.B + (int64_t)(n0 + dn + r16) * p.ldb) + 8 * q;
+  const char* br[NB];
+  [[maybe_unused]] const uint8_t* sr[NB];
+#pragma unroll
+  for (int x = 0; x < NB; ++x) {
+    const bool second = pair && (NB == 1 ? r16 >= 8 : x >= HALF);   // a lane of the second kind
+    const int r = NB == 1 ? (pair ? r16 & 7 : r16) : pair ? 16 * (x % HALF) + r16 : 16 * x + r16;
+    const int row = n0 + r + (second && EPI != EPI_SWIGLU ? dn : 0);
+    const bool b2 = EPI == EPI_SWIGLU && second;
+    if constexpr (Q4) {
+      // a block of columns behind the last (plain stores): the last one's, not stored
+      const int64_t blk = (int64_t)min(row >> 4, (p.N - 1) >> 4) * KT;
+      br[x] = (const char*)(b2 ? qv.codes2 : qv.codes) + blk * kQuantBlock + (row & 15) * 16 + q * 256;
+      sr[x] = (b2 ? qv.scales2 : qv.scales) + blk * kQuantScales + (row & 15) * 4;
+    } else {
+      br[x] = (const char*)((b2 ? p.B2 : p.B) + (int64_t)row * p.ldb + 8 * q);
+    }
   }
-  u32x4_t bw[2][U][NB][2], aw[2][U][MB][2];
+  constexpr int BH = Q4 ? 1 : HS;                       // loads of a weight piece
+  u32x4_t bw[2][U][NB][BH], aw[2][U][MB][HS];
+  [[maybe_unused]] uint32_t sw[2][U][NB];
   // a stage: up to U pieces of K from c0 on, below hi
   constexpr int kStep = SPLIT ? 1 : W;
-  auto load_b = [&](int c0, int hi, u32x4_t (&b)[U][NB][2]) {
+  auto load_b = [&](int c0, int hi, int st) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + u * kStep;
       if (c >= hi) continue;   // uniform over the wave
 #pragma unroll
-      for (int x = 0; x < NB; ++x)
+      for (int x = 0; x < NB; ++x) {
+        if constexpr (Q4) {
+          bw[st][u][x][0] = __builtin_nontemporal_load(
+              reinterpret_cast<const u32x4_t*>(br[x] + (int64_t)c * kQuantBlock));
+          sw[st][u][x] = *reinterpret_cast<const uint32_t*>(sr[x] + (int64_t)c * kQuantScales);
+        } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          b[u][x][h] = __builtin_nontemporal_load(
-              reinterpret_cast<const u32x4_t*>(br[x] + (int64_t)c * BK + 32 * h));
+          for (int h = 0; h < HS; ++h)
+            bw[st][u][x][h] = __builtin_nontemporal_load(
+                reinterpret_cast<const u32x4_t*>(br[x] + 2 * ((int64_t)c * BK + 32 * h)));
+        }
+      }
     }
   };
   if constexpr (SPLIT) {
-    if (wave < nseg) load_b(lo_of(wave), hi_of(wave), bw[0]);
+    if (wave < nseg) load_b(lo_of(wave), hi_of(wave), 0);
   } else {
-    load_b(wave, KT, bw[0]);
+    load_b(wave, KT, 0);
   }
 
   // the rows: active rows, then (row list) the rows that exited before the
   // layer, in one ballot of at most 64 token rows
   int M = p.M_dev ? min(*p.M_dev, rl.exit_layer ? rl.max_act : p.M_max) : p.M_max;
+  if constexpr (Q4 && EPI == EPI_STORE) M = min(M - m0, kDirectRows);
   if (rl.ticket && blockIdx.x == 0 && threadIdx.x < 2) rl.ticket[threadIdx.x] = 0ull;
   const bf16* ar[MB];
   if (rl.exit_layer) {
@@ -171,7 +225,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
     for (int i = 0; i < G; ++i)
       if (pre[i].m >= M) pre[i].row = 0;
   }
-  auto load_a = [&](int c0, int hi, u32x4_t (&a)[U][MB][2]) {
+  auto load_a = [&](int c0, int hi, int st) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + u * kStep;
@@ -180,29 +234,49 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
       for (int y = 0; y < MB; ++y)
         if (y == 0 || 16 * y < M) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            a[u][y][h] = *reinterpret_cast<const u32x4_t*>(ar[y] + (int64_t)c * BK + 32 * h);
+          for (int h = 0; h < HS; ++h) {
+            if constexpr (Q4) {
+              // rows that are not there and K behind the last are zeros (the codes there
+              // are too, but not what memory holds: 0 times NaN); a lane without a row
+              // loads nothing
+              aw[st][u][y][h] = u32x4_t{0, 0, 0, 0};
+              if (16 * y + r16 < M && c * KP + 32 * h + 8 * q < p.K)
+                aw[st][u][y][h] =
+                    *reinterpret_cast<const u32x4_t*>(ar[y] + (int64_t)c * KP + 32 * h);
+            } else {
+              aw[st][u][y][h] = *reinterpret_cast<const u32x4_t*>(ar[y] + (int64_t)c * KP + 32 * h);
+            }
+          }
         }
     }
   };
   if constexpr (SPLIT) {
-    if (wave < nseg) load_a(lo_of(wave), hi_of(wave), aw[0]);
+    if (wave < nseg) load_a(lo_of(wave), hi_of(wave), 0);
   } else {
-    load_a(wave, KT, aw[0]);
+    load_a(wave, KT, 0);
   }
   // the epilogue's inputs
 #pragma unroll
   for (int i = 0; i < G; ++i) {
     DirPre& e = pre[i];
     const int t = wave + W * i, x = t % XB;
-    const int kind = per == 8 ? q >> 1 : x;           // of a pair
-    e.out = t < MB * XB && e.m < M && !(EPI == EPI_SWIGLU && kind);
-    e.n = n0 + (per == 8 ? (EPI == EPI_SWIGLU ? 0 : kind * dn) + 4 * (q & 1) : x * dn + 4 * q);
+    const int kind = per == 8 ? q >> 1 : x / HALF;    // of a pair
+    e.out = t < MB * XB && e.m < M && !(EPI == EPI_SWIGLU && per == 8 && kind);
+    e.n = n0 + (per == 8 ? (EPI == EPI_SWIGLU ? 0 : kind * dn) + 4 * (q & 1)
+                         : (HALF == 1 ? x * dn
+                            : rope     ? kind * dn + 16 * (x % HALF)
+                                       : 16 * x) + 4 * q);
     e.sc = 1.0f;
     e.bias = bf16x4_t{0, 0, 0, 0};
     if (!e.out) continue;
     if (p.row_scale) e.sc = p.row_scale[e.m];
-    if (p.bias) e.bias = *reinterpret_cast<const bf16x4_t*>(p.bias + e.n);
+    if (p.bias && Q4 && EPI == EPI_STORE) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (e.n + c < p.N) e.bias[c] = p.bias[e.n + c];
+    } else if (p.bias) {
+      e.bias = *reinterpret_cast<const bf16x4_t*>(p.bias + e.n);
+    }
     if constexpr (EPI == EPI_RESID)
       e.resid = *reinterpret_cast<const bf16x4_t*>(p.resid + (int64_t)e.row * p.ldc + e.n);
     if constexpr (EPI == EPI_QKV) {
@@ -222,31 +296,39 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
 #pragma unroll
     for (int x = 0; x < NB; ++x) acc[y][x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  auto step = [&](int c0, int hi, u32x4_t (&a)[U][MB][2], u32x4_t (&b)[U][NB][2]) {
+  auto step = [&](int c0, int hi, int st) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (c0 + u * kStep >= hi) continue;
 #pragma unroll
-      for (int y = 0; y < MB; ++y)
-        if (y == 0 || 16 * y < M) {
+      for (int h = 0; h < HS; ++h) {
+        bf16x8_t bv[NB];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const bf16x8_t av = __builtin_bit_cast(bf16x8_t, a[u][y][h]);
+        for (int x = 0; x < NB; ++x) {
+          if constexpr (Q4)
+            bv[x] = quant_expand(bw[st][u][x][0][h], sw[st][u][x] >> (8 * h));
+          else
+            bv[x] = __builtin_bit_cast(bf16x8_t, bw[st][u][x][h]);
+        }
+#pragma unroll
+        for (int y = 0; y < MB; ++y)
+          if (y == 0 || 16 * y < M) {
+            const u32x4_t a = aw[st][u][y][h];
 #pragma unroll
             for (int x = 0; x < NB; ++x)
               acc[y][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  __builtin_bit_cast(bf16x8_t, b[u][x][h]), av, acc[y][x], 0, 0, 0);
+                  bv[x], __builtin_bit_cast(bf16x8_t, a), acc[y][x], 0, 0, 0);
             if (row_norm) {
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const float lo = __uint_as_float(a[u][y][h][e] << 16);
-                const float hi = __uint_as_float(a[u][y][h][e] & 0xffff0000u);
+                const float lo = __uint_as_float(a[e] << 16);
+                const float hi = __uint_as_float(a[e] & 0xffff0000u);
                 ss[y] = fmaf(lo, lo, ss[y]);
                 ss[y] = fmaf(hi, hi, ss[y]);
               }
             }
           }
-        }
+      }
     }
   };
   auto hand_over = [&](int s) {   // the sums of segment s
@@ -280,20 +362,20 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
       int s1 = s, c1 = c;
       next(s1, c1);
       if (s1 < nseg) {
-        load_b(c1, hi_of(s1), bw[1]);
-        load_a(c1, hi_of(s1), aw[1]);
+        load_b(c1, hi_of(s1), 1);
+        load_a(c1, hi_of(s1), 1);
       }
-      step(c, hi_of(s), aw[0], bw[0]);
+      step(c, hi_of(s), 0);
       if (s1 != s) finish(s);
       s = s1;
       c = c1;
       if (s >= nseg) break;
       next(s1, c1);
       if (s1 < nseg) {
-        load_b(c1, hi_of(s1), bw[0]);
-        load_a(c1, hi_of(s1), aw[0]);
+        load_b(c1, hi_of(s1), 0);
+        load_a(c1, hi_of(s1), 0);
       }
-      step(c, hi_of(s), aw[1], bw[1]);
+      step(c, hi_of(s), 1);
       if (s1 != s) finish(s);
       s = s1;
       c = c1;
@@ -305,16 +387,16 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
 #pragma unroll 1
     for (int it = 0; it < iters; it += 2) {
       if (it + 1 < iters) {
-        load_b(at(it + 1), KT, bw[1]);
-        load_a(at(it + 1), KT, aw[1]);
+        load_b(at(it + 1), KT, 1);
+        load_a(at(it + 1), KT, 1);
       }
-      step(at(it), KT, aw[0], bw[0]);
+      step(at(it), KT, 0);
       if (it + 1 < iters) {
         if (it + 2 < iters) {
-          load_b(at(it + 2), KT, bw[0]);
-          load_a(at(it + 2), KT, aw[0]);
+          load_b(at(it + 2), KT, 0);
+          load_a(at(it + 2), KT, 0);
         }
-        step(at(it + 1), KT, aw[1], bw[1]);
+        step(at(it + 1), KT, 1);
       }
     }
     hand_over(wave);   // a wave without pieces: zeros
@@ -362,6 +444,10 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
     float v[4] = {x4.x * sc + bx[0], x4.y * sc + bx[1], x4.z * sc + bx[2], x4.w * sc + bx[3]};
     bf16x4_t o;
     if constexpr (EPI == EPI_STORE) {
+      if constexpr (Q4) {
+        store_any(p, m0 + e.m, e.n, v);
+        continue;
+      }
       if (p.c_f32) {
         *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.C) + (int64_t)e.m * p.ldc + e.n) =
             make_float4(v[0], v[1], v[2], v[3]);
@@ -370,7 +456,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
     }
     bf16* dst = reinterpret_cast<bf16*>(p.C) + (int64_t)(EPI == EPI_RESID ? e.row : e.m) * p.ldc + e.n;
     if constexpr (EPI == EPI_SWIGLU) {
-      const float4 y4 = per == 8 ? sum(y, lane ^ 32) : sum(y * NB + NB - 1, lane);
+      const float4 y4 = per == 8 ? sum(y, lane ^ 32) : sum(y * NB + x + NB / 2, lane);
       const float u[4] = {y4.x * sc, y4.y * sc, y4.z * sc, y4.w * sc};
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[c] = f2bf(silu(v[c]) * u[c]);
@@ -379,8 +465,8 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
       dst = (sec == 0 ? p.q_out + (int64_t)e.m * p.d_q
                       : (sec == 2 ? p.v_cache : p.k_cache) + (int64_t)e.slot * p.d_q) + cin;
       if (rope && sec != 2) {
-        const bool first = per == 8 ? q < 2 : x == 0;
-        const float4 y4 = per == 8 ? sum(y, lane ^ 32) : sum(y * NB + (x ^ (NB - 1)), lane);
+        const bool first = per == 8 ? q < 2 : x < HALF;
+        const float4 y4 = per == 8 ? sum(y, lane ^ 32) : sum(y * NB + (x ^ (NB / 2)), lane);
         const float4 by = bias4(p.bias, first ? e.n + dn : e.n - dn);
         const float w[4] = {y4.x * sc + by.x, y4.y * sc + by.y, y4.z * sc + by.z, y4.w * sc + by.w};
         const float cv[4] = {e.cs.x, e.cs.y, e.cs.z, e.cs.w};
@@ -411,9 +497,9 @@ int split_segments(const SkSplit& sp) {
   return sp.KT % sp.U == 0 ? sp.KT / sp.U : (sp.KT + sp.U - 2) / sp.U + 1;
 }
 
-template <int EPI, int NB, int MB, int W, int U, bool SPLIT>
+template <int EPI, int NB, int MB, int W, int U, bool SPLIT, bool Q4 = false>
 adept_status dir_launch(const GP& p, const RowList& rl, int row_norm, const char* name,
-                        hipStream_t s) {
+                        hipStream_t s, const QuantView& qv = QuantView{}) {
   SkSplit sp{};
   int parts = W;
   if (SPLIT) {
@@ -423,13 +509,15 @@ adept_status dir_launch(const GP& p, const RowList& rl, int row_norm, const char
   const size_t red = (size_t)parts * MB * NB * 1024;
   static bool attr_set = false;
   if (SPLIT || red > 48 * 1024)
-    ADEPT_TRY(lds_limit((const void*)gemm_direct_kernel<EPI, NB, MB, W, U, SPLIT>,
+    ADEPT_TRY(lds_limit((const void*)gemm_direct_kernel<EPI, NB, MB, W, U, SPLIT, Q4>,
                         SPLIT ? kSplitLds : red, &attr_set, "gemm_direct LDS limit"));
   const int cols = EPI == EPI_SWIGLU ? 8 * NB : 16 * NB;
+  const dim3 grid(ceil_div(p.N, cols),
+                  Q4 && EPI == EPI_STORE ? ceil_div(p.M_max, kDirectRows) : 1);
   {
     TimedLaunch tl(name ? name : "gemm_direct", s);
-    hipLaunchKernelGGL((gemm_direct_kernel<EPI, NB, MB, W, U, SPLIT>), dim3(p.N / cols),
-                       dim3(64 * W), red, s, p, rl, row_norm, sp);
+    hipLaunchKernelGGL((gemm_direct_kernel<EPI, NB, MB, W, U, SPLIT, Q4>), grid, dim3(64 * W), red,
+                       s, p, rl, row_norm, sp, qv);
   }
   return launch_status("gemm_direct");
 }
@@ -458,6 +546,20 @@ adept_status dir_rows(const GP& p, const RowList& rl, int row_norm, const char* 
                 : dir_launch<EPI, 1, 2, 8, SPLIT ? 4 : 2, SPLIT>(p, rl, row_norm, name, s);
   return wide ? dir_launch<EPI, 2, 4, 8, 1, SPLIT>(p, rl, row_norm, name, s)
               : dir_launch<EPI, 1, 4, 8, SPLIT ? 2 : 1, SPLIT>(p, rl, row_norm, name, s);
+}
+
+// Weights in 4 bits.
+template <int EPI>
+adept_status quant_rows(const GP& p, const RowList& rl, int row_norm, const QuantView& qv,
+                        const char* name, hipStream_t s) {
+  const int M = rl.exit_layer ? rl.n_tok : p.M_max;
+  const int tiles = ceil_div(EPI == EPI_SWIGLU ? 2 * p.N : p.N, 16);
+  if (M <= 16) return dir_launch<EPI, 1, 1, 8, 2, false, true>(p, rl, row_norm, name, s, qv);
+  if (M <= 32)
+    return tiles >= 512 ? dir_launch<EPI, 2, 2, 8, 1, false, true>(p, rl, row_norm, name, s, qv)
+                        : dir_launch<EPI, 1, 2, 8, 1, false, true>(p, rl, row_norm, name, s, qv);
+  return tiles >= 512 ? dir_launch<EPI, 2, 4, 8, 1, false, true>(p, rl, row_norm, name, s, qv)
+                      : dir_launch<EPI, 1, 4, 8, 1, false, true>(p, rl, row_norm, name, s, qv);
 }
 
 }  // namespace
@@ -491,6 +593,7 @@ bool gemm_direct_split_fits(int M_max, int N, int K, int epi) {
 }
 
 bool gemm_direct_fits(const GemmArgs& g) {
+  if (g.quant.codes) return g.M_max > 0 && (g.M_max <= kDirectRows || g.epi == EPI_STORE);
   if (g.few_rows == kFewSkinny) return false;
   if (g.few_rows == kFewSplit) return !g.rope_cos && gemm_direct_split_fits(g.M_max, g.N, g.K, g.epi);
   return gemm_direct_fits(g.M_max, g.epi == EPI_SWIGLU ? 2 * g.N : g.N, g.K, g.epi);
@@ -500,6 +603,16 @@ adept_status gemm_direct(const GemmArgs& g, hipStream_t s) {
   const GP p = to_gp(g);
   const RowList rl = g.list ? *g.list : RowList{};
   const int rn = g.row_norm ? 1 : 0;
+  if (g.quant.codes) {
+    switch (g.epi) {
+      case EPI_STORE: return quant_rows<EPI_STORE>(p, rl, rn, g.quant, g.name, s);
+      case EPI_QKV: return quant_rows<EPI_QKV>(p, rl, rn, g.quant, g.name, s);
+      case EPI_RESID: return quant_rows<EPI_RESID>(p, rl, rn, g.quant, g.name, s);
+      case EPI_SWIGLU: return quant_rows<EPI_SWIGLU>(p, rl, rn, g.quant, g.name, s);
+      case EPI_GELU_TANH: return quant_rows<EPI_GELU_TANH>(p, rl, rn, g.quant, g.name, s);
+      default: set_error("gemm: 4-bit weights without this epilogue"); return ADEPT_E_INVALID;
+    }
+  }
   if (g.few_rows == kFewSplit) {
     switch (g.epi) {
       case EPI_QKV: return dir_rows<EPI_QKV, true>(p, rl, rn, g.name, s);

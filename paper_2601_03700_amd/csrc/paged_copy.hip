@@ -1,0 +1,91 @@
+// Pages of a paged cache copied to other pages in all layers at once
+// (adept_paged_copy): a forked sequence's open page, a compacted cache.
+//
+// Bound by HBM: every byte is read and written once.  A workgroup moves kPart bytes
+// of one page of one layer's K or V, all of its loads in flight before its first
+// store.
+#include <algorithm>
+
+#include "paged.h"
+
+namespace adept {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;
+constexpr int kPart = kThreads * 16 * kUnroll;   // bytes
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+struct CopyArgs {
+  char *k, *v;
+  uint8_t *k_scale, *v_scale;     // nullable
+  const int32_t *src, *dst, *n_tokens, *n_pages;
+  int max_pages, cache_pages, page_size, row_bytes, heads, parts, layers;
+};
+
+__global__ __launch_bounds__(kThreads) void paged_copy_kernel(CopyArgs a) {
+  // the parts of a page next to each other, then K and V, layers, pages
+  const uint32_t blk = blockIdx.x;
+  const int part = blk % a.parts;
+  const uint32_t rest = blk / a.parts;
+  const int which = rest & 1;
+  const int layer = (rest >> 1) % a.layers, i = (rest >> 1) / a.layers;
+  if (a.n_pages && i >= *a.n_pages) return;
+  const int src = a.src[i], dst = a.dst[i];
+  if ((unsigned)src >= (unsigned)a.cache_pages || (unsigned)dst >= (unsigned)a.cache_pages ||
+      src == dst)
+    return;
+  const int tokens = a.n_tokens ? min(max(a.n_tokens[i], 0), a.page_size) : a.page_size;
+  const int64_t page = (int64_t)a.page_size * a.row_bytes;
+  char* base = (which ? a.v : a.k) + (int64_t)layer * a.cache_pages * page;
+  const char* from = base + src * page;
+  char* to = base + dst * page;
+  const int64_t bytes = (int64_t)tokens * a.row_bytes, lo = (int64_t)part * kPart;
+  u32x4_t w[kUnroll];
+#pragma unroll
+  for (int e = 0; e < kUnroll; ++e) {
+    const int64_t at = lo + (e * kThreads + threadIdx.x) * 16;
+    if (at < bytes) w[e] = *reinterpret_cast<const u32x4_t*>(from + at);
+  }
+#pragma unroll
+  for (int e = 0; e < kUnroll; ++e) {
+    const int64_t at = lo + (e * kThreads + threadIdx.x) * 16;
+    if (at < bytes) *reinterpret_cast<u32x4_t*>(to + at) = w[e];
+  }
+  if (!a.k_scale || part != 0) return;
+  uint8_t* scale = (which ? a.v_scale : a.k_scale) +
+                   (int64_t)layer * a.cache_pages * a.page_size * a.heads;
+  const int64_t s0 = (int64_t)src * a.page_size * a.heads, d0 = (int64_t)dst * a.page_size * a.heads;
+  const int n = tokens * a.heads;
+  for (int e = threadIdx.x; e < n; e += kThreads) scale[d0 + e] = scale[s0 + e];
+}
+
+}  // namespace
+}  // namespace adept
+
+using namespace adept;
+
+extern "C" adept_status adept_paged_copy(const adept_paged_kv* kv, int n_layers,
+                                         const int32_t* src_page, const int32_t* dst_page,
+                                         const int32_t* n_tokens, const int32_t* n_pages,
+                                         int max_pages, void* stream) {
+  ADEPT_TRY(paged_check("paged_copy", kv && kv->dtype == ADEPT_KV_F32 ? ADEPT_F32 : ADEPT_BF16, kv));
+  ADEPT_REQUIRE(n_layers >= 1 && max_pages >= 0, "paged_copy: bad sizes");
+  if (max_pages == 0) return ADEPT_OK;
+  ADEPT_REQUIRE(src_page && dst_page, "paged_copy: NULL list of pages");
+  CopyArgs a{};
+  a.k = (char*)kv->k; a.v = (char*)kv->v;
+  const bool fp8 = kv->dtype == ADEPT_KV_FP8;
+  if (fp8) { a.k_scale = kv->k_scale; a.v_scale = kv->v_scale; }
+  a.src = src_page; a.dst = dst_page; a.n_tokens = n_tokens; a.n_pages = n_pages;
+  a.max_pages = max_pages; a.cache_pages = kv->n_pages; a.page_size = kv->page_size;
+  a.heads = kv->n_kv_heads; a.layers = n_layers;
+  a.row_bytes = kv->n_kv_heads * kv->head_dim * (fp8 ? 1 : kv->dtype == ADEPT_KV_F32 ? 4 : 2);
+  a.parts = ceil_div((long)kv->page_size * a.row_bytes, kPart);
+  const int64_t blocks = (int64_t)max_pages * n_layers * 2 * a.parts;
+  ADEPT_REQUIRE(blocks < 1 << 24,   // a grid's bound: 256 GiB
+                "paged_copy: %d pages of %d layers are too many for a call", max_pages, n_layers);
+  ADEPT_LAUNCH(paged_copy_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, as_stream(stream), a);
+  return launch_status("paged_copy");
+}
