@@ -630,6 +630,25 @@ adept_status adept_layer_step_paged(const adept_layer_args* a, const adept_paged
                                     const int32_t* page_table, int max_pages,
                                     const int32_t* cache_slot, int layer, void* stream);
 
+/* adept_layer_step (kv NULL) or adept_layer_step_paged (else) with the layers' weights
+ * in 4 bits as well: each matrix of adept_layer_args stacked over the layers as
+ * adept_quant_pack lays it out (after the folding of gains).  Passes of at
+ * most 64 token rows (n_tok: decode, the verification of a few drafts) read them,
+ * the weights' bytes being what bounds those; larger passes and the K/V generation
+ * after a layer read a's weights, which have to hold the same values
+ * (adept_quant_unpack).  bf16; up is unused in the GPT2 family.
+ *  workspace: adept_layer_quant_workspace_bytes(a, w, kv, max_pages). */
+typedef struct { const void* codes; const void* scales; } adept_quant_mat;
+typedef struct {       /* (host); gate: W_fc, down: W_proj in the GPT2 family */
+  adept_quant_mat qkv, o, gate, up, down;
+} adept_quant_layers;
+size_t adept_layer_quant_workspace_bytes(const adept_layer_args* a, const adept_quant_layers* w,
+                                         const adept_paged_kv* kv, int max_pages);
+adept_status adept_layer_step_quant(const adept_layer_args* a, const adept_quant_layers* w,
+                                    const adept_paged_kv* kv, const int32_t* page_table,
+                                    int max_pages, const int32_t* cache_slot, int layer,
+                                    void* stream);
+
 /* Folds a norm gain into the weight matrices that consume the normalised
  * vector, in place: w[l][o][c] *= gain[l][c] for l < n_mats, o < rows,
  * c < cols, rounded to dtype; matrix l starts at w + l*mat_stride, its gain at

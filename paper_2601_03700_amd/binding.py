@@ -84,6 +84,15 @@ class PagedKv(ctypes.Structure):
                 ("n_pages", _i32), ("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp)]
 
 
+class QuantMat(ctypes.Structure):
+    _fields_ = [("codes", _vp), ("scales", _vp)]
+
+
+class QuantLayers(ctypes.Structure):
+    _fields_ = [("qkv", QuantMat), ("o", QuantMat), ("gate", QuantMat), ("up", QuantMat),
+                ("down", QuantMat)]
+
+
 _SIGS = {
     "adept_abi_version": (_i32, []),
     "adept_last_error": (ctypes.c_char_p, []),
@@ -142,6 +151,11 @@ _SIGS = {
                                                _i32]),
     "adept_layer_step_paged": (_i32, [ctypes.POINTER(LayerArgs), ctypes.POINTER(PagedKv), _vp, _i32,
                                       _vp, _i32, _vp]),
+    "adept_layer_quant_workspace_bytes": (_sz, [ctypes.POINTER(LayerArgs),
+                                                ctypes.POINTER(QuantLayers),
+                                                ctypes.POINTER(PagedKv), _i32]),
+    "adept_layer_step_quant": (_i32, [ctypes.POINTER(LayerArgs), ctypes.POINTER(QuantLayers),
+                                      ctypes.POINTER(PagedKv), _vp, _i32, _vp, _i32, _vp]),
     "adept_embed": (_i32, [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
     "adept_final_logits": (_i32, [_i32, _i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _vp,
                                   _i32, _vp, _vp, _vp, _vp, _vp]),
@@ -713,18 +727,55 @@ def _layers_from(kv):
     return kv.layers
 
 
+def _paged_step(what, args, kv, page_table, cache_slot):
+    if page_table.dim() != 2 or page_table.shape[0] < args.n_seq:
+        raise AdeptError(f"{what}: page_table must be [n_seq, max_pages]")
+    if cache_slot is not None and cache_slot.numel() < args.n_tok:
+        raise AdeptError(f"{what}: one slot for each row")
+    if _layers_from(kv) < args.n_layers:
+        raise AdeptError(f"{what}: {args.n_layers} layers, the cache has "
+                         f"{kv.layers} from the described one on")
+    return _i32_ptrs(what, _device_of(what, kv), page_table, cache_slot)
+
+
+def quant_layers(args: LayerArgs, qkv, o, gate, up, down):
+    """Descriptor of the layers' weights in 4 bits (QuantWeights of all layers each; up None in the
+    GPT2 family), which it holds."""
+    N, D, dq, F = args.n_layers, args.d_model, args.n_heads * args.head_dim, args.d_ff
+    q = QuantLayers()
+    for name, w, n, k in (("qkv", qkv, 3 * dq, D), ("o", o, D, dq), ("gate", gate, F, D),
+                          ("up", up, F, D), ("down", down, D, F)):
+        if w is None and name == "up" and args.family == FAMILY_GPT2:
+            continue
+        if w is None or (w.n, w.k) != (n, k) or w.n_mats < N:
+            raise AdeptError(f"quant_layers: {name} must be {N} matrices of {n} x {k}")
+        setattr(q, name, QuantMat(w.codes.data_ptr(), w.scales.data_ptr()))
+    q.weights = (qkv, o, gate, up, down)
+    return q
+
+
+def layer_quant_workspace_bytes(args: LayerArgs, weights, kv=None, max_pages=0):
+    return lib().adept_layer_quant_workspace_bytes(
+        ctypes.byref(args), ctypes.byref(weights), ctypes.byref(kv) if kv is not None else None,
+        max_pages)
+
+
+def layer_step_quant(args: LayerArgs, weights, layer, kv=None, page_table=None, cache_slot=None,
+                     stream=None):
+    """layer_step (kv None) or layer_step_paged with the weights in 4 bits as well (quant_layers)."""
+    tp = cp = None
+    if kv is not None:
+        tp, cp = _paged_step("layer_step_quant", args, kv, page_table, cache_slot)
+    _check(lib().adept_layer_step_quant(ctypes.byref(args), ctypes.byref(weights),
+                                        ctypes.byref(kv) if kv is not None else None, tp,
+                                        page_table.shape[1] if kv is not None else 0, cp, layer,
+                                        stream_handle(stream)), "adept_layer_step_quant")
+
+
 def layer_step_paged(args: LayerArgs, kv, page_table, layer, cache_slot=None, stream=None):
     """layer_step over a paged cache; kv: paged_kv of its first layer, the others behind it;
     page_table int32 [n_seq, max_pages]; cache_slot int32, one for each row (8-bit caches)."""
-    if page_table.dim() != 2 or page_table.shape[0] < args.n_seq:
-        raise AdeptError("layer_step_paged: page_table must be [n_seq, max_pages]")
-    if cache_slot is not None and cache_slot.numel() < args.n_tok:
-        raise AdeptError("layer_step_paged: one slot for each row")
-    if _layers_from(kv) < args.n_layers:
-        raise AdeptError(f"layer_step_paged: {args.n_layers} layers, the cache has "
-                         f"{kv.layers} from the described one on")
-    dev = _device_of("layer_step_paged", kv)
-    tp, cp = _i32_ptrs("layer_step_paged", dev, page_table, cache_slot)
+    tp, cp = _paged_step("layer_step_paged", args, kv, page_table, cache_slot)
     _check(lib().adept_layer_step_paged(ctypes.byref(args), ctypes.byref(kv), tp,
                                         page_table.shape[1], cp, layer, stream_handle(stream)),
            "adept_layer_step_paged")

@@ -48,10 +48,17 @@ struct LayerWs {
   size_t total;
 };
 
+// Whether the step reads its weights in 4 bits: up to the few rows of one kernel each.
+// Passes of more rows read the bf16 weights, which hold the same values.
+bool step_quant(const adept_layer_args* a, const adept_quant_layers* qw) {
+  return qw && a->dtype == ADEPT_BF16 && a->n_tok <= kDirectRows;
+}
+
 // Whether all GEMMs of the step run as one kernel each (gemm_direct.hip), form
 // the RMSNorm factor of their rows (and the fused schedule's row list)
 // themselves, and leave the exit test to exit_compact.
-bool step_direct(const adept_layer_args* a) {
+bool step_direct(const adept_layer_args* a, const adept_quant_layers* qw) {
+  if (step_quant(a, qw)) return true;
   const int dq = a->n_heads * a->head_dim, D = a->d_model, F = a->d_ff, n = a->n_tok;
   const bool gpt2 = a->family == ADEPT_FAMILY_GPT2;
   return a->dtype == ADEPT_BF16 && gemm_direct_fits(n, 3 * dq, D, EPI_QKV) &&
@@ -60,7 +67,8 @@ bool step_direct(const adept_layer_args* a) {
          gemm_direct_fits(n, D, F, EPI_RESID);
 }
 
-LayerWs carve(const adept_layer_args* a, void* base, const PagedStep* pg) {
+LayerWs carve(const adept_layer_args* a, void* base, const PagedStep* pg,
+              const adept_quant_layers* qw) {
   LayerWs w{};
   char* p = (char*)base;
   size_t off = 0;
@@ -87,7 +95,7 @@ LayerWs carve(const adept_layer_args* a, void* base, const PagedStep* pg) {
   w.prompt = p + off; off += align256(w.prompt_bytes);
   w.hsm_bytes = a->hsm ? adept_hsm_workspace_bytes(a->d_model, a->n_tok) : 0;
   w.hsm = p + off; off += align256(w.hsm_bytes);
-  if (step_direct(a)) {
+  if (step_direct(a, qw)) {
     w.ticket = (unsigned long long*)(p + off);
     off += 256;
   } else if (a->dtype == ADEPT_BF16 && a->n_tok <= 64) {
@@ -315,7 +323,8 @@ adept_status attend_step(const adept_layer_args* a, const PagedStep* pg, int lay
                                a->attn_tiles ? kPagedTiles : kPagedSteps, s);
 }
 
-adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* pg, void* stream);
+adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* pg,
+                        const adept_quant_layers* qw, void* stream);
 
 }  // namespace
 }  // namespace adept
@@ -324,25 +333,25 @@ using namespace adept;
 
 extern "C" size_t adept_layer_workspace_bytes(const adept_layer_args* a) {
   if (!a) return 0;
-  return carve(a, nullptr, nullptr).total;
+  return carve(a, nullptr, nullptr, nullptr).total;
 }
 
 extern "C" size_t adept_layer_paged_workspace_bytes(const adept_layer_args* a,
                                                     const adept_paged_kv* kv, int max_pages) {
   if (!a || !kv) return 0;
   const PagedStep pg{kv, nullptr, max_pages, nullptr};
-  return carve(a, nullptr, &pg).total;
+  return carve(a, nullptr, &pg, nullptr).total;
 }
 
 extern "C" adept_status adept_layer_step(const adept_layer_args* a, int layer, void* stream) {
   ADEPT_REQUIRE(a != nullptr, "layer_step: args is NULL");
-  return layer_step(a, layer, nullptr, stream);
+  return layer_step(a, layer, nullptr, nullptr, stream);
 }
 
-extern "C" adept_status adept_layer_step_paged(const adept_layer_args* a, const adept_paged_kv* kv,
-                                               const int32_t* page_table, int max_pages,
-                                               const int32_t* cache_slot, int layer, void* stream) {
-  ADEPT_REQUIRE(a != nullptr, "layer_step_paged: args is NULL");
+namespace adept {
+namespace {
+adept_status check_paged_step(const adept_layer_args* a, const adept_paged_kv* kv,
+                              const int32_t* page_table, int max_pages, const int32_t* cache_slot) {
   ADEPT_TRY(paged_check("layer_step_paged", (adept_dtype)a->dtype, kv));
   ADEPT_REQUIRE(kv->n_kv_heads == a->n_heads && kv->head_dim == a->head_dim,
                 "layer_step_paged: the cache's heads are not the layer's");
@@ -361,13 +370,49 @@ extern "C" adept_status adept_layer_step_paged(const adept_layer_args* a, const 
     ADEPT_REQUIRE(a->k_cache == kv->k && a->v_cache == kv->v && a->n_slots == paged_slots(*kv),
                   "layer_step_paged: the arguments' cache is not the paged one");
   }
-  const PagedStep pg{kv, page_table, max_pages, cache_slot};
-  return layer_step(a, layer, &pg, stream);
+  return ADEPT_OK;
 }
+}  // namespace
+}  // namespace adept
+
+extern "C" adept_status adept_layer_step_paged(const adept_layer_args* a, const adept_paged_kv* kv,
+                                               const int32_t* page_table, int max_pages,
+                                               const int32_t* cache_slot, int layer, void* stream) {
+  ADEPT_REQUIRE(a != nullptr, "layer_step_paged: args is NULL");
+  ADEPT_TRY(check_paged_step(a, kv, page_table, max_pages, cache_slot));
+  const PagedStep pg{kv, page_table, max_pages, cache_slot};
+  return layer_step(a, layer, &pg, nullptr, stream);
+}
+
+extern "C" size_t adept_layer_quant_workspace_bytes(const adept_layer_args* a,
+                                                    const adept_quant_layers* w,
+                                                    const adept_paged_kv* kv, int max_pages) {
+  if (!a || !w) return 0;
+  const PagedStep pg{kv, nullptr, max_pages, nullptr};
+  return carve(a, nullptr, kv ? &pg : nullptr, w).total;
+}
+
+extern "C" adept_status adept_layer_step_quant(const adept_layer_args* a, const adept_quant_layers* w,
+                                               const adept_paged_kv* kv, const int32_t* page_table,
+                                               int max_pages, const int32_t* cache_slot, int layer,
+                                               void* stream) {
+  ADEPT_REQUIRE(a != nullptr && w != nullptr, "layer_step_quant: args is NULL");
+  ADEPT_REQUIRE(a->dtype == ADEPT_BF16, "layer_step_quant: bf16 passes only");
+  const adept_quant_mat* mats[5] = {&w->qkv, &w->o, &w->gate, &w->down, &w->up};
+  for (int i = 0; i < (a->family == ADEPT_FAMILY_GPT2 ? 4 : 5); ++i)
+    ADEPT_REQUIRE(mats[i]->codes && mats[i]->scales && aligned16(mats[i]->codes) &&
+                      aligned16(mats[i]->scales),
+                  "layer_step_quant: codes and scales must be 16-byte aligned");
+  if (kv) ADEPT_TRY(check_paged_step(a, kv, page_table, max_pages, cache_slot));
+  const PagedStep pg{kv, page_table, max_pages, cache_slot};
+  return layer_step(a, layer, kv ? &pg : nullptr, w, stream);
+}
+
 
 namespace adept {
 namespace {
-adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* pg, void* stream) {
+adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* pg,
+                        const adept_quant_layers* qw, void* stream) {
   const adept_dtype dt = (adept_dtype)a->dtype;
   ADEPT_REQUIRE(dt == ADEPT_F32 || dt == ADEPT_BF16, "layer_step: bad dtype");
   const int N = a->n_layers, D = a->d_model, H = a->n_heads, hd = a->head_dim, F = a->d_ff;
@@ -397,12 +442,12 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
                 "layer_step: GLOBAL/BOTH metrics need inertia");
   ADEPT_REQUIRE(!a->hsm || (dt == ADEPT_BF16 && a->exit.metric != ADEPT_SIM_LOCAL && a->inertia),
                 "layer_step: the mapper needs bf16 and the inertia (GLOBAL or BOTH metric)");
-  const size_t need = carve(a, nullptr, pg).total;
+  const size_t need = carve(a, nullptr, pg, qw).total;
   if (!a->workspace || a->workspace_bytes < need) {
     set_error("layer_step: workspace of %zu bytes needed", need);
     return ADEPT_E_WORKSPACE;
   }
-  LayerWs ws = carve(a, a->workspace, pg);
+  LayerWs ws = carve(a, a->workspace, pg, qw);
   hipStream_t s = as_stream(stream);
   const int in = (layer - 1) & 1, out = layer & 1;
   const int32_t* act = a->active[in];
@@ -422,6 +467,21 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
   void* kc = (void*)off(a->k_cache, li * a->n_slots * dq);
   void* vc = (void*)off(a->v_cache, li * a->n_slots * dq);
 
+  // the same matrices in 4 bits
+  const bool quant = step_quant(a, qw);
+  auto packed = [&](const adept_quant_mat& m, int n, int k) {
+    return adept_quant_mat{(const char*)m.codes + li * (int64_t)adept_quant_codes_bytes(n, k),
+                           (const char*)m.scales + li * (int64_t)adept_quant_scales_bytes(n, k)};
+  };
+  auto quant_of = [&](GemmArgs& x, const adept_quant_mat& m, const adept_quant_mat* m2) {
+    const adept_quant_mat p1 = packed(m, x.N, x.K);
+    x.quant = QuantView{(const uint8_t*)p1.codes, (const uint8_t*)p1.scales, nullptr, nullptr};
+    if (!m2) return;
+    const adept_quant_mat p2 = packed(*m2, x.N, x.K);
+    x.quant.codes2 = (const uint8_t*)p2.codes;
+    x.quant.scales2 = (const uint8_t*)p2.scales;
+  };
+
   // fused schedule: the QKV GEMM's rows are the active rows, then the rows
   // that exited earlier in the pass (their K/V at this layer, Eq. 9)
   const bool fused = a->kv_fused != 0;
@@ -431,7 +491,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
   // at most 64 rows: all GEMMs of the step direct, or all on the skinny path, whose
   // epilogues carry the next norm and the exit test (width 512, MLP 4096, 64
   // rows, only the gate/up projection skinny: 132 us two layers, all 119)
-  const bool direct = step_direct(a);
+  const bool direct = step_direct(a, qw);
   const int few = direct ? kFewAny : kFewSkinny;
   const bool tail = direct && exit_compact_fits(a->exit, D, maxn, false) && a->exit.prompt_level == 0;
   // fused schedule: the row list and the QKV rows' norm (the RMSNorm
@@ -509,6 +569,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     g.q_out = a->q_buf; g.k_cache = kc; g.v_cache = vc; g.name = "gemm_qkv";
     g.skinny_ws = ws.skinny; g.skinny_ws_bytes = ws.skinny_bytes;
     g.few_rows = few;
+    if (quant) quant_of(g, qw->qkv, nullptr);
     if (tail) g.list = &list;
     ADEPT_TRY(gemm(dt, g, s));
     // 3. attention over the mixed cache
@@ -521,6 +582,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     go.C = a->h[out]; go.ldc = D; go.resid = a->h[in]; go.rows = act; go.name = "gemm_o";
     go.skinny_ws = ws.skinny; go.skinny_ws_bytes = ws.skinny_bytes;
     go.few_rows = few;
+    if (quant) quant_of(go, qw->o, nullptr);
     // 5. LN2: on the skinny path the projection's epilogue writes it
     if (gemm_skinny_row_norm(go)) {
       go.ln_out = ws.xnorm;
@@ -538,6 +600,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     gf.C = a->ffn_act; gf.ldc = F; gf.name = "gemm_fc";
     gf.skinny_ws = ws.skinny; gf.skinny_ws_bytes = ws.skinny_bytes;
     gf.few_rows = few;
+    if (quant) quant_of(gf, qw->gate, nullptr);
     ADEPT_TRY(gemm(dt, gf, s));
     // 7. second MLP projection + bias + residual (in place on h[out])
     GemmArgs gd{};
@@ -547,6 +610,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     gd.C = a->h[out]; gd.ldc = D; gd.resid = a->h[out]; gd.rows = act; gd.name = "gemm_proj";
     gd.skinny_ws = ws.skinny; gd.skinny_ws_bytes = ws.skinny_bytes;
     gd.few_rows = few;
+    if (quant) quant_of(gd, qw->down, nullptr);
     ADEPT_TRY(exit_in_epilogue(gd));
     ADEPT_TRY(gemm(dt, gd, s));
   } else if (qmax > 0) {
@@ -575,6 +639,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     g.q_out = a->q_buf; g.k_cache = kc; g.v_cache = vc; g.name = "gemm_qkv";
     g.skinny_ws = ws.skinny; g.skinny_ws_bytes = ws.skinny_bytes;
     g.few_rows = few;
+    if (quant) quant_of(g, qw->qkv, nullptr);
     if (norm_in_gemm(g))
       g.row_norm = true;
     else if (!rinv_fused)
@@ -590,6 +655,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     go.C = a->h[out]; go.ldc = D; go.resid = a->h[in]; go.rows = act; go.name = "gemm_o";
     go.skinny_ws = ws.skinny; go.skinny_ws_bytes = ws.skinny_bytes;
     go.few_rows = few;
+    if (quant) quant_of(go, qw->o, nullptr);
     // 5. pre-FFN RMSNorm (gain folded into W_gate / W_up): its row factors
     //    come from the projection's epilogue on the skinny path
     if (dt == ADEPT_BF16 && gemm_skinny_row_norm(go)) {
@@ -605,6 +671,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     gu.C = a->ffn_act; gu.ldc = F; gu.name = "gemm_gate_up";
     gu.skinny_ws = ws.skinny; gu.skinny_ws_bytes = ws.skinny_bytes;
     gu.few_rows = few;
+    if (quant) quant_of(gu, qw->gate, &qw->up);
     if (norm_in_gemm(gu))
       gu.row_norm = true;
     else if (!go.rinv_out)
@@ -617,6 +684,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
     gd.C = a->h[out]; gd.ldc = D; gd.resid = a->h[out]; gd.rows = act; gd.name = "gemm_down";
     gd.skinny_ws = ws.skinny; gd.skinny_ws_bytes = ws.skinny_bytes;
     gd.few_rows = few;
+    if (quant) quant_of(gd, qw->down, nullptr);
     ADEPT_TRY(exit_in_epilogue(gd));
     ADEPT_TRY(run_gemm(dt, gd, ws.gemm_tmp, s));
   }

@@ -15,9 +15,10 @@ step runs one new token per sequence against the cache the prefill (and
 earlier steps) filled, with generated entries for every skipped layer.
 
 The cache is either a KVCache (s_max slots for each sequence) or a
-PagedKVCache: pages that sequences take as they grow and give back, in the
-model's type or in 8 bits.  Over either, a prompt can be run in pieces
-(prefill with start).
+PagedKVCache: pages that sequences take as they grow, share and give back, in
+the model's type or in 8 bits.  Over either, a prompt can be run in pieces
+(prefill with start), and drafted tokens can be verified (verify,
+generate_drafted).
 """
 from __future__ import annotations
 
@@ -54,7 +55,10 @@ class PagedKVCache:
     no place.  A pass over an "fp8" cache holds its own rows' K and V of all layers in the
     model's type beside it: long prompts are better run in pieces (prefill with start).  Its
     decode passes need the K/V generation inside the layers (kv_fused, bf16 models); without
-    it they run as prompts do, their attention in tiles: right, and slower."""
+    it they run as prompts do, their attention in tiles: right, and slower.
+
+    Sequences may share pages (fork): a page goes back when the last of them gives it up, and a
+    pass that writes into a shared one gets a copy of it first (reserve with start)."""
 
     def __init__(self, n_layers, n_heads, head_dim, n_seq, n_pages, page_size, max_pages, kv_dtype,
                  device):
@@ -71,6 +75,8 @@ class PagedKVCache:
         self.page_table = torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=device)
         self._free = list(range(n_pages - 1, -1, -1))
         self._pages = [[] for _ in range(n_seq)]
+        self._users = [0] * n_pages        # sequences that a page belongs to
+        self.shared_pages = 0              # pages that belong to several
         self.kv = self.layer_kv(1)
 
     @property
@@ -80,6 +86,10 @@ class PagedKVCache:
     @property
     def s_max(self):
         return self.max_pages * self.page_size
+
+    @property
+    def n_pages(self):
+        return len(self._users)
 
     @property
     def free_pages(self):
@@ -95,33 +105,149 @@ class PagedKVCache:
         if not 0 <= seq < self.n_seq:
             raise ValueError(f"sequence {seq}: the cache has {self.n_seq}")
 
-    def reserve(self, lengths):
-        """Pages for lengths[b] tokens of sequence b (a dict or one number for all); raises
+    def _take(self, n):
+        pages = [self._free.pop() for _ in range(n)]
+        for p in pages:
+            self._users[p] = 1
+        return pages
+
+    def _give(self, pages):
+        """Pages that a sequence no longer has; the ones that no other has are free."""
+        for p in reversed(pages):
+            self._users[p] -= 1
+            if self._users[p] == 0:
+                self._free.append(p)
+            elif self._users[p] == 1:
+                self.shared_pages -= 1
+
+    def _write_table(self, seq):
+        row = self._pages[seq]
+        self.page_table[seq, :len(row)] = torch.tensor(row, dtype=torch.int32)
+
+    def _copy(self, src, dst, n_tokens=None):
+        """Pages of all layers (binding.paged_copy)."""
+        if src:
+            up = lambda x: torch.tensor(x, dtype=torch.int32, device=self.k.device)
+            B.paged_copy(self.kv, self.k.shape[0], up(src), up(dst),
+                         None if n_tokens is None else up(n_tokens))
+
+    def reserve(self, lengths, start=None):
+        """Pages for lengths[b] tokens of sequence b (a dict or one number for all); start[b]: the
+        position from which on they are going to be written (a dict or one number; None: behind
+        the tokens that are shared), whose pages a sequence then gets for itself.  Raises
         ValueError, with nothing taken, where they do not fit."""
         if not isinstance(lengths, dict):
             lengths = {b: int(lengths) for b in range(self.n_seq)}
         for b in lengths:
             self._check_sequence(b)
-        more = {b: -(-n // self.page_size) - len(self._pages[b]) for b, n in lengths.items()}
         for b, n in lengths.items():
             if not 0 <= n <= self.s_max:
                 raise ValueError(f"{n} tokens of sequence {b}: a sequence holds up to {self.s_max}")
+        more = {b: -(-n // self.page_size) - len(self._pages[b]) for b, n in lengths.items()}
         need = sum(m for m in more.values() if m > 0)
-        if need > len(self._free):
-            raise ValueError(f"{need} more pages needed, {len(self._free)} free")
+        own = []                            # (sequence, which of its pages)
+        if start is not None:
+            users = list(self._users)
+            for b, n in lengths.items():
+                first = int(start[b] if isinstance(start, dict) else start)
+                last = min(-(-n // self.page_size), len(self._pages[b]))
+                for i in range(max(first, 0) // self.page_size, last):
+                    if users[self._pages[b][i]] > 1:
+                        users[self._pages[b][i]] -= 1
+                        own.append((b, i))
+        if need + len(own) > len(self._free):
+            raise ValueError(f"{need + len(own)} more pages needed, {len(self._free)} free")
+        new = self._take(len(own))
+        self._copy([self._pages[b][i] for b, i in own], new)
+        for (b, i), page in zip(own, new):
+            self._give([self._pages[b][i]])
+            self._pages[b][i] = page
+            self.page_table[b, i] = page
         for b, m in more.items():
             if m > 0:
-                new = [self._free.pop() for _ in range(m)]
+                new = self._take(m)
                 at = len(self._pages[b])
                 self._pages[b] += new
                 self.page_table[b, at:at + m] = torch.tensor(new, dtype=torch.int32)
 
     def release(self, seq):
         """Gives the sequence's pages back (its tokens are gone)."""
+        self.truncate(seq, 0)
+
+    def truncate(self, seq, length):
+        """Keeps the first `length` tokens of a sequence and gives back the pages behind them."""
         self._check_sequence(seq)
-        self._free += reversed(self._pages[seq])
-        self._pages[seq] = []
-        self.page_table[seq].fill_(-1)
+        if length < 0:
+            raise ValueError(f"{length} tokens of sequence {seq}")
+        keep = -(-length // self.page_size)
+        self._give(self._pages[seq][keep:])
+        self._pages[seq] = self._pages[seq][:keep]
+        self.page_table[seq, keep:].fill_(-1)
+
+    def fork(self, src, dst, length):
+        """The sequences dst (one or several, without pages) continue from the first `length`
+        tokens of sequence src: they share its full pages, and each gets a copy of what is
+        used of the open one.  Raises ValueError, with nothing taken, where that does not fit."""
+        dst = [dst] if isinstance(dst, int) else list(dst)
+        for b in (src, *dst):
+            self._check_sequence(b)
+        if src in dst or len(set(dst)) < len(dst) or any(self._pages[b] for b in dst):
+            raise ValueError("a fork goes to other sequences, each without pages of its own")
+        full, left = divmod(length, self.page_size)
+        if length < 0 or full + (left > 0) > len(self._pages[src]):
+            raise ValueError(f"{length} tokens: sequence {src} has pages for "
+                             f"{len(self._pages[src]) * self.page_size}")
+        if left and len(dst) > len(self._free):
+            raise ValueError(f"{len(dst)} more pages needed, {len(self._free)} free")
+        new = self._take(len(dst)) if left else []
+        if new:
+            self._copy([self._pages[src][full]] * len(new), new, [left] * len(new))
+        for k, b in enumerate(dst):
+            self._pages[b] = self._pages[src][:full] + new[k:k + 1]
+            for p in self._pages[b][:full]:
+                self._users[p] += 1
+                self.shared_pages += self._users[p] == 2
+            self._write_table(b)
+
+    def _move(self, n_pages):
+        """Pages from the n_pages-th on into free ones below; how many."""
+        src = [p for p in range(n_pages, self.n_pages) if self._users[p]]
+        holes = sorted(p for p in self._free if p < n_pages)[:len(src)]
+        self._copy(src, holes)
+        to = dict(zip(src, holes))
+        for p, q in to.items():
+            self._users[q], self._users[p] = self._users[p], 0
+        for b, pages in enumerate(self._pages):
+            if any(p in to for p in pages):
+                self._pages[b] = [to.get(p, p) for p in pages]
+                self._write_table(b)
+        self._free = [p for p in range(self.n_pages - 1, -1, -1) if not self._users[p]]
+        return len(src)
+
+    def compact(self):
+        """Moves the pages in use to the front of the cache; how many were moved."""
+        return self._move(self.n_pages - len(self._free))
+
+    def resize(self, n_pages):
+        """Another number of pages: more of them, or memory given back after a peak (pages in use
+        behind the new end are moved first).  Descriptors of the old tensors are no longer the
+        cache's.  Raises ValueError where more pages are in use."""
+        used = self.n_pages - len(self._free)
+        if n_pages < used or n_pages < 1:
+            raise ValueError(f"{n_pages} pages, {used} in use")
+        if n_pages < self.n_pages:
+            self._move(n_pages)
+        keep = min(n_pages, self.n_pages) * self.page_size
+        for name in ("k", "v", "k_scale", "v_scale"):
+            old = getattr(self, name)
+            if old is not None:
+                new = torch.empty((old.shape[0], (n_pages + 1) * self.page_size, *old.shape[2:]),
+                                  dtype=old.dtype, device=old.device)
+                new[:, :keep] = old[:, :keep]
+                setattr(self, name, new)
+        self._users = (self._users + [0] * (n_pages - self.n_pages))[:n_pages]
+        self._free = [p for p in range(n_pages - 1, -1, -1) if not self._users[p]]
+        self.kv = self.layer_kv(1)
 
     def slots(self, pos, seq):
         """Slots (int32) of tokens at pos of sequences seq, both int32 device tensors; the last
@@ -185,8 +311,13 @@ class DecoderModel:
     """
 
     def __init__(self, shape, weights, dtype="bf16", device="cuda", rope_max_pos=4096,
-                 hsm_weights=None, kv_fused=True):
+                 hsm_weights=None, kv_fused=True, quant=False):
         self.shape = shape
+        # the layers' matrices and the head in 4 bits (bf16): passes of at most 64 tokens read
+        # those, larger ones the bf16 matrices, which then hold the same values
+        self.quant, self._quant_struct = None, None
+        if quant and dtype != "bf16":
+            raise ValueError("weights in 4 bits go with a bf16 model")
         # decode passes in bf16: exited rows' K/V from the later layers' QKV
         # GEMMs (True) or one grouped generation after the last layer (False)
         self.kv_fused = kv_fused
@@ -207,6 +338,8 @@ class DecoderModel:
             if dtype != "bf16" or hsm_weights is not None:
                 raise ValueError("the LayerNorm family runs in bf16 without a mapper")
             self._init_gpt2(weights, up)
+            if quant:
+                self._quantise()
             return
         self.b_qkv = self.b_o = self.b_fc = self.b_proj = None
         if isinstance(weights.get("layers"), list):
@@ -244,6 +377,27 @@ class DecoderModel:
         self.rope_cos = torch.empty((rope_max_pos, half), dtype=torch.float32, device=dev)
         self.rope_sin = torch.empty_like(self.rope_cos)
         B.rope_table(rope_max_pos, shape.head_dim, shape.rope_theta, self.rope_cos, self.rope_sin)
+        if quant:
+            self._quantise()
+
+    def _quantise(self):
+        """The matrices in 4 bits, and the bf16 ones rounded to what those hold."""
+        self.quant = {}
+        for name in ("w_qkv", "w_o", "w_gate", "w_up", "w_down"):
+            w = getattr(self, name)
+            if w is None:
+                self.quant[name] = None
+                continue
+            q = self.quant[name] = B.quant_weights(w.shape[1], w.shape[2], self.device, w.shape[0])
+            held = torch.empty_like(w)      # the given matrices keep their values
+            for i in range(w.shape[0]):
+                B.quant_pack(w[i], q, i)
+                B.quant_unpack(q, held[i], i)
+            setattr(self, name, held)
+        head = self.quant["lm_head"] = B.quant_weights(*self.lm_head.shape, self.device)
+        B.quant_pack(self.lm_head, head)
+        self.lm_head = torch.empty_like(self.lm_head)
+        B.quant_unpack(head, self.lm_head)
 
     def _init_gpt2(self, weights, up):
         s = self.shape
@@ -365,8 +519,15 @@ class DecoderModel:
             a.k_cache, a.v_cache, a.n_slots = B.ptr(cache.k), B.ptr(cache.v), cache.n_slots
         a.q_buf, a.attn_out, a.ffn_act = B.ptr(st.q_buf), B.ptr(st.attn_out), B.ptr(st.ffn_act)
         a.hsm = ctypes.addressof(self._hsm_struct) if self._hsm_struct is not None else None
-        need = (B.layer_paged_workspace_bytes(a, cache.kv, cache.max_pages) if paged
-                else B.layer_workspace_bytes(a))
+        if self.quant is not None:
+            if self._quant_struct is None:
+                self._quant_struct = B.quant_layers(a, *(self.quant[n] for n in (
+                    "w_qkv", "w_o", "w_gate", "w_up", "w_down")))
+            need = B.layer_quant_workspace_bytes(a, self._quant_struct, cache.kv if paged else None,
+                                                 cache.max_pages if paged else 0)
+        else:
+            need = (B.layer_paged_workspace_bytes(a, cache.kv, cache.max_pages) if paged
+                    else B.layer_workspace_bytes(a))
         if st.workspace is None or st.workspace.numel() < need:
             st.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
         a.workspace, a.workspace_bytes = B.ptr(st.workspace), st.workspace.numel()
@@ -403,7 +564,10 @@ class DecoderModel:
         B.token_init(n, s.n_layers, s.d_model, st.active[0], st.counts, st.exit_layer, st.inertia)
         args = self.layer_args(st, cache, cfg, attn_tiles)
         for i in range(1, s.n_layers + 1):
-            if paged:
+            if self.quant is not None:
+                B.layer_step_quant(args, self._quant_struct, i, cache.kv if paged else None,
+                                   cache.page_table if paged else None, st.cache_slot)
+            elif paged:
                 B.layer_step_paged(args, cache.kv, cache.page_table, i, st.cache_slot)
             else:
                 B.layer_step(args, i)
@@ -416,7 +580,14 @@ class DecoderModel:
         n_rows = torch.tensor([nr], dtype=torch.int32, device=self.device)
         logits = torch.empty((nr, s.vocab), dtype=torch.float32, device=self.device)
         xn = torch.empty((nr, s.d_model), dtype=self.tdt, device=self.device)
-        if self.gpt2:
+        # (the bf16 GEMMs take a vocabulary that is a multiple of 64)
+        if self.quant is not None and (nr <= 64 or s.vocab % 64):
+            gain, bias = ((self.final_ln_g, self.final_ln_b) if self.gpt2
+                          else (self.final_norm, None))
+            B.final_logits_quant(s.d_model, s.vocab, s.ln_eps if self.gpt2 else s.rms_eps, st.h[0],
+                                 st.h[1], st.exit_layer, rows, n_rows, nr, gain, bias,
+                                 self.quant["lm_head"], xn, logits)
+        elif self.gpt2:
             B.final_logits_layernorm(s.d_model, s.vocab, s.ln_eps, st.h[0], st.h[1],
                                      st.exit_layer, rows, n_rows, nr, self.final_ln_g,
                                      self.final_ln_b, self.lm_head, xn, logits)
@@ -442,7 +613,7 @@ class DecoderModel:
         seq = torch.arange(Bn, dtype=torch.int32, device=dev).repeat_interleave(T)
         self._check_positions(pos, cache.s_max, pos_max=start + T - 1)
         if isinstance(cache, PagedKVCache):
-            cache.reserve({b: start + T for b in range(Bn)})
+            cache.reserve({b: start + T for b in range(Bn)}, start)
         fl = None
         if isinstance(force_layer, torch.Tensor):
             fl = force_layer.reshape(-1).to(dev, torch.int32)
@@ -467,11 +638,113 @@ class DecoderModel:
         self._check_sequences(cache, n)
         self._check_positions(pos, cache.s_max, pos_max)
         if isinstance(cache, PagedKVCache):
-            at = [pos_max] * n if pos_max is not None else pos.tolist()
-            cache.reserve({b: int(p) + 1 for b, p in enumerate(at)})
+            self._reserve(cache, pos, pos_max, 1)
         rows = torch.arange(n, dtype=torch.int32, device=dev)
         return self.token_pass(ids.to(torch.int32), pos.to(torch.int32), seq, cache, cfg,
                                force_layer, False, rows, on_layer)
+
+    @staticmethod
+    def _reserve(cache, pos, pos_max, n):
+        """Pages for n new tokens from pos[b] on (at most pos_max, where the host knows no more: it
+        reads pos back only if a page might be shared)."""
+        if pos_max is None or cache.shared_pages:
+            at = {b: int(p) for b, p in enumerate(pos.tolist())}
+            top = (lambda p: p) if pos_max is None else (lambda p: max(p, pos_max))
+            cache.reserve({b: top(p) + n for b, p in at.items()}, at)
+        else:
+            cache.reserve({b: pos_max + n for b in range(int(pos.shape[0]))})
+
+    # --------------------------------------------------------------- drafts
+    def draw(self, logits, u, temperature=None):
+        """A token of each row of logits [n, V] from random numbers u [n] in [0, 1); temperature [n]
+        f32 (None: 1; 0: the largest)."""
+        return self.verify_logits(logits[:, None], None, torch.empty(
+            (logits.shape[0], 0), dtype=torch.int32, device=logits.device), u[:, None],
+            temperature)[0][:, 0]
+
+    def verify_logits(self, target, draft, tokens, u, temperature=None, n_draft=None):
+        """binding.verify_drafts: (tokens [n, g+1], kept [n])."""
+        n, rows, V = target.shape
+        i32 = dict(dtype=torch.int32, device=target.device)
+        out, kept = torch.empty((n, rows), **i32), torch.empty(n, **i32)
+        ws = torch.empty(B.verify_drafts_workspace_bytes(n, rows - 1, V), dtype=torch.uint8,
+                         device=target.device)
+        B.verify_drafts(target, draft, tokens, u.contiguous(), out, kept, n_draft, temperature, ws)
+        return out, kept
+
+    def verify(self, cache, last, drafts, pos, cfg, u, draft_logits=None, temperature=None,
+               pos_max=None):
+        """One pass over each sequence's last token (at pos[b], not yet in the cache) and its drafts
+        [n, g] behind it, and their verification: (tokens [n, g+1], kept [n], pass result).  The
+        cache then holds the last token and the drafts; those that were not kept are written
+        over by what comes next.  draft_logits [n, g, V] f32 (None: the drafts have no
+        probabilities); u [n, g+1]; temperature [n]; pos_max: the largest pos, when known on the
+        host."""
+        n, g = drafts.shape
+        self._check_sequences(cache, n)
+        top = pos_max if pos_max is not None else (int(pos.max()) if n else 0)
+        self._check_positions(pos, cache.s_max, top + g)
+        if isinstance(cache, PagedKVCache):
+            self._reserve(cache, pos, pos_max, g + 1)
+        i32 = dict(dtype=torch.int32, device=self.device)
+        ids = torch.cat([last.to(torch.int32)[:, None], drafts.to(torch.int32)], 1)
+        at = pos.to(torch.int32)[:, None] + torch.arange(g + 1, **i32)
+        seq = torch.arange(n, **i32).repeat_interleave(g + 1)
+        rows = torch.arange(n * (g + 1), **i32)
+        res = self.token_pass(ids.reshape(-1), at.reshape(-1), seq, cache, cfg, None, True, rows)
+        out, kept = self.verify_logits(res.logits.view(n, g + 1, -1), draft_logits,
+                                       drafts.to(torch.int32).contiguous(), u, temperature)
+        return out, kept, res
+
+    def generate_drafted(self, ids, n_steps, cfg, draft_cfg, n_draft=4, temperature=0.0,
+                         generator=None, cache=None):
+        """n_steps tokens of each prompt of ids [B, T], drafted by passes that leave early
+        (draft_cfg) and verified n_draft at a time by one pass under cfg, whose distribution the
+        tokens have (temperature 0: its largest logits).  generator: of the random numbers, on the
+        model's device.  cache: an empty one of either kind with room for T + n_steps + n_draft
+        tokens of each sequence.  Returns (tokens [B, n_steps], how many drafts were kept, how many
+        were made, cache)."""
+        if n_draft < 1 or n_steps < 0:
+            raise ValueError(f"{n_steps} tokens, {n_draft} drafts at a time")
+        ids_t = torch.as_tensor(np.asarray(ids) if not isinstance(ids, torch.Tensor) else ids)
+        n, T = ids_t.shape
+        dev = self.device
+        i32 = dict(dtype=torch.int32, device=dev)
+        end = T + n_steps - 1               # of the last token that is put into the cache
+        if cache is None:
+            cache = self.new_cache(n, T + n_steps + n_draft)
+        self._check_positions(ids_t, cache.s_max, end + n_draft)
+        temp = torch.full((n,), float(temperature), dtype=torch.float32, device=dev)
+        rand = lambda *d: torch.rand(d, generator=generator, device=dev)
+        res, _ = self.prefill(ids_t, cfg, logits="last", cache=cache)
+        # out[:, n_steps] takes what a finished sequence still draws
+        out = torch.zeros((n, n_steps + n_draft + 1), **i32)
+        out[:, 0] = self.draw(res.logits, rand(n), temp)
+        have = torch.ones(n, **i32)         # tokens of each sequence
+        kept_all, made, least, most = 0, 0, 1, 1
+        i = torch.arange(n_draft + 1, device=dev)
+        while least < n_steps:
+            pos = T - 1 + have              # of the last token
+            last = out.gather(1, have.long()[:, None] - 1)[:, 0]
+            tok, drafts, logits = last, [], []
+            for k in range(n_draft):
+                step = self.decode_step(cache, tok, pos + k, draft_cfg,
+                                        pos_max=T - 1 + most + k)
+                tok = self.draw(step.logits, rand(n), temp)
+                drafts.append(tok)
+                logits.append(step.logits)
+            toks, kept, _ = self.verify(cache, last, torch.stack(drafts, 1), pos, cfg,
+                                        rand(n, n_draft + 1), torch.stack(logits, 1), temp,
+                                        pos_max=T - 1 + most)
+            at = have[:, None] + i
+            out.scatter_(1, torch.where((i <= kept[:, None]) & (at < n_steps), at,
+                                        n_steps + n_draft).long(), toks)
+            live = have < n_steps
+            kept_all += int((kept * live).sum())
+            made += n_draft * int(live.sum())
+            have = (have + kept + 1).clamp(max=n_steps)
+            least, most = int(have.min()), int(have.max())
+        return out[:, :n_steps], kept_all, made, cache
 
     def greedy(self, logits):
         n, V = logits.shape
