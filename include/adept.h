@@ -441,7 +441,7 @@ adept_status adept_paged_copy(const adept_paged_kv* kv, int n_layers, const int3
  *  kept ones comes from the distribution proportional to max(p_i - q_i, 0) where
  *  draft i was the first one not kept, and from p_g where all g were.  It is the
  *  first token whose running sum (in ascending order of the tokens) exceeds u_last
- *  times the whole sum.  Where p_i - q_i leaves nothing, p_i.
+ *  times the whole sum.  Where p_i - q_i leaves nothing (above 2^-40 of p_i), p_i.
  *
  *  target [n_seq][max_draft+1][vocab] (dt), rows target_stride elements apart;
  *  draft [n_seq][max_draft][vocab] (dt), rows draft_stride apart, nullable: then

@@ -11,10 +11,12 @@
 // border.  The vector units take 64-bit products and sums at the rate of unpacked
 // 32-bit ones, and one exponential is about 20 of them.
 //
-// Three kernels: the maximum and the sum of every row's chunks (all of the traffic:
-// the logits once); the decision of each sequence, and what the row of its next
-// token holds, chunk by chunk; the token itself, by the chunks' sums and then inside
-// one chunk.
+// Two kernels.  The first takes the maximum and the sum of every row, 1024 logits a
+// wave: all of the traffic, each logit once.  The second has a few workgroups for each
+// sequence: every one makes the decision for itself (some partial sums from L2, less
+// than one more kernel costs), takes its share of what p - q holds, and the last of them
+// draws the token, by the shares' sums and then inside one.
+#include <algorithm>
 #include <climits>
 
 #include "common.h"
@@ -22,28 +24,25 @@
 namespace adept {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kPer = 8;                      // logits of a thread
-constexpr int kChunk = kThreads * kPer;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kRowPer = 16;                  // logits of a lane in the first kernel
+constexpr int kChunk = 64 * kRowPer;         // of a wave
+constexpr int kPer = 8;
+constexpr int kTile = kThreads * kPer;       // tokens of a share in the second
+constexpr int kBlock = 64;                   // drafts that are decided at once
 
-// A chunk of a row: its maximum (NaN left out), that value's first index, and the
-// sum of exp((l - max) / T).
+// A chunk of a row, or a row: its maximum (NaN left out), that value's first index
+// (where it is asked for) and the sum of the weights.
 struct Part {
   double sum;
   float top;
   int at;
 };
 enum PickMode { kPickGreedy, kPickRow, kPickRest, kPickOthers };
-// What the next token of a sequence is drawn from.
-struct Pick {
-  double p_total, q_total;
-  float p_top, q_top;
-  int kept, mode, at, gone;   // at: the greedy token; gone: the token left out (kPickOthers)
-};
 
 template <typename T>
 struct Verify {
-  int n_seq, g, vocab, chunks;
+  int n_seq, g, vocab, chunks, tiles, groups;   // groups: workgroups of a sequence
   const T* target;
   int64_t t_stride;
   const T* draft;               // nullable
@@ -52,17 +51,17 @@ struct Verify {
   const float *temperature, *u;
   int32_t *out, *kept;
   Part* part;                   // [n_seq (g + 1) target rows, n_seq g draft rows][chunks]
-  double* rest;                 // [n_seq][chunks]
-  Pick* pick;                   // [n_seq]
+  uint64_t* rest;               // [n_seq][tiles], doubles
+  unsigned* ticket;             // [n_seq]
 
   __device__ __forceinline__ int drafts(int b) const {
     return n_draft ? min(max(n_draft[b], 0), g) : g;
   }
-  // 1 / T; 0 or less: the largest logit
-  __device__ __forceinline__ double inverse(int b, bool* greedy) const {
+  // log2(e) / T; 0 or less: the largest logit
+  __device__ __forceinline__ double slope(int b, bool* greedy) const {
     const float t = temperature ? temperature[b] : 1.0f;
     *greedy = !(t > 0.0f);
-    return *greedy ? 1.0 : 1.0 / (double)t;
+    return *greedy ? 1.0 : 1.4426950408889634 / (double)t;
   }
   __device__ __forceinline__ const T* target_row(int b, int i) const {
     return target + ((int64_t)b * (g + 1) + i) * t_stride;
@@ -85,53 +84,90 @@ __device__ __forceinline__ int lead_of(const T* row) {
   return (int)(((uintptr_t)row & 15) / sizeof(T));
 }
 
-// e^x for x <= 0: x = n ln 2 + r, |r| <= ln 2 / 2, and the series of e^r up to r^12
-// (what is left out is below 2e-16 of it).
-__device__ __forceinline__ double exp_neg(double x) {
-  if (x < -745.0) return 0.0;
-  const double n = rint(x * 1.4426950408889634);
-  double r = fma(n, -0.6931471805599453, x);
-  r = fma(n, -2.3190468138462996e-17, r);      // ln 2 less its 64-bit value
-  double s = 1.0 / 479001600.0;
-  s = fma(s, r, 1.0 / 39916800.0);
-  s = fma(s, r, 1.0 / 3628800.0);
-  s = fma(s, r, 1.0 / 362880.0);
-  s = fma(s, r, 1.0 / 40320.0);
-  s = fma(s, r, 1.0 / 5040.0);
-  s = fma(s, r, 1.0 / 720.0);
-  s = fma(s, r, 1.0 / 120.0);
-  s = fma(s, r, 1.0 / 24.0);
-  s = fma(s, r, 1.0 / 6.0);
-  s = fma(s, r, 0.5);
-  s = fma(s, r, 1.0);
-  s = fma(s, r, 1.0);
+// 2^x for x <= 0, 0 for NaN: 2^n 2^f with n = rint(x), and 2^f by the polynomial of
+// degree 10 through the Chebyshev points of [-1/2, 1/2] (off by 3e-16 of it).
+__device__ __forceinline__ double exp2_neg(double x) {
+  x = fmax(x, -1100.0);   // 2^-1100 is 0
+  const double n = rint(x), f = x - n;
+  double s = 7.072585949269223e-09;
+  s = fma(s, f, 1.0208690299958306e-07);
+  s = fma(s, f, 1.321544258792169e-06);
+  s = fma(s, f, 1.5252657260200837e-05);
+  s = fma(s, f, 0.0001540353044173605);
+  s = fma(s, f, 0.0013333558230164974);
+  s = fma(s, f, 0.009618129107606888);
+  s = fma(s, f, 0.05550410866444772);
+  s = fma(s, f, 0.24022650695910097);
+  s = fma(s, f, 0.69314718055995);
+  s = fma(s, f, 1.0);
   return ldexp(s, (int)n);
 }
 
-// The weight of a logit in a row whose largest is `top`: none for NaN and -inf; where
-// the largest is +inf, the infinite ones share the row.
-__device__ __forceinline__ double weight(float l, float top, double inv) {
-  if (!(l > -INFINITY)) return 0.0;
-  if (top == INFINITY) return l == INFINITY ? 1.0 : 0.0;
-  return exp_neg(((double)l - (double)top) * inv);
+// The weight of a logit in a row whose largest is `top`, exp((l - top) / T): none for NaN
+// and -inf; where the largest is +inf, the infinite ones share the row.
+__device__ __forceinline__ double weight(float l, float top, double slope) {
+  if (top == INFINITY) return l == INFINITY ? 1.0 : 0.0;   // uniform over a row
+  return exp2_neg(((double)l - (double)top) * slope);
+}
+
+// Scans over a wave by DPP moves: a shuffle through LDS is ten times the latency, and
+// the second kernel is a chain of them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_f64(double v) {   // 0 where there is no lane to read
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)u, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double lane_f64(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)u, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(u >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+constexpr int kShr = 0x110, kBcast15 = 0x142, kBcast31 = 0x143;   // row_shr, row_bcast
+// the running sum up to and with a lane
+__device__ __forceinline__ double scan_f64(double v) {
+  v += dpp_f64<kShr + 1, 0xf>(v);
+  v += dpp_f64<kShr + 2, 0xf>(v);
+  v += dpp_f64<kShr + 4, 0xf>(v);
+  v += dpp_f64<kShr + 8, 0xf>(v);
+  v += dpp_f64<kBcast15, 0xa>(v);
+  v += dpp_f64<kBcast31, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ double sum_f64(double v) { return lane_f64(scan_f64(v), 63); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_f32(float v) {     // -inf where there is no lane to read
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0xff800000u, __float_as_uint(v), CTRL, ROWS, 0xf,
+                                                     false));
+}
+__device__ __forceinline__ float max_f32(float v) {
+  v = fmaxf(v, dpp_f32<kShr + 1, 0xf>(v));
+  v = fmaxf(v, dpp_f32<kShr + 2, 0xf>(v));
+  v = fmaxf(v, dpp_f32<kShr + 4, 0xf>(v));
+  v = fmaxf(v, dpp_f32<kShr + 8, 0xf>(v));
+  v = fmaxf(v, dpp_f32<kBcast15, 0xa>(v));
+  v = fmaxf(v, dpp_f32<kBcast31, 0xc>(v));
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
 // Block sums, the same in every thread.
 __device__ __forceinline__ double block_sum(double v, double* sh) {
-  v = wave_sum_f64(v);
+  v = sum_f64(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
   double s = sh[0];
-  for (int w = 1; w < kThreads / 64; ++w) s += sh[w];
+  for (int w = 1; w < kWaves; ++w) s += sh[w];
   return s;
 }
 
-__device__ __forceinline__ void load_vec(const float* p, float (&x)[4]) {
+__device__ __forceinline__ void load_vec(const float* p, float* x) {
   const float4 w = *reinterpret_cast<const float4*>(p);
   x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
 }
-__device__ __forceinline__ void load_vec(const bf16* p, float (&x)[8]) {
+__device__ __forceinline__ void load_vec(const bf16* p, float* x) {
   const uint4 w = *reinterpret_cast<const uint4*>(p);
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -141,279 +177,320 @@ __device__ __forceinline__ void load_vec(const bf16* p, float (&x)[8]) {
   }
 }
 
+// The first index of the largest value over a wave.
+__device__ __forceinline__ void wave_first_max(float& top, int& at) {
+  for (int o = 32; o > 0; o >>= 1) {
+    const float ot = __shfl_xor(top, o, 64);
+    const int oa = __shfl_xor(at, o, 64);
+    if (ot > top || (ot == top && oa < at)) { top = ot; at = oa; }
+  }
+}
+
 template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_rows_kernel(Verify<T> a) {
-  constexpr int VEC = 16 / sizeof(T), J = kPer / VEC;
-  __shared__ double sh[kThreads / 64];
-  __shared__ float tops[kThreads / 64];
-  __shared__ int ats[kThreads / 64];
+__global__ __launch_bounds__(kThreads) void verify_rows_kernel(Verify<T> a, int rows) {
+  constexpr int VEC = 16 / sizeof(T), J = kRowPer / VEC;
+  const int lane = threadIdx.x & 63;
+  const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
   const int rows_t = a.n_seq * (a.g + 1);
-  const int r = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks;
+  const int r = unit / a.chunks, c = unit % a.chunks;
+  if (r >= rows) return;
   const bool of_target = r < rows_t;
-  const int per = of_target ? a.g + 1 : a.g;
-  const int b = (of_target ? r : r - rows_t) / per, i = (of_target ? r : r - rows_t) % per;
+  const int per = of_target ? a.g + 1 : a.g, at_row = of_target ? r : r - rows_t;
+  const int b = at_row / per, i = at_row % per;
   if (i >= a.drafts(b) + (of_target ? 1 : 0)) return;
   bool greedy;
-  const double inv = a.inverse(b, &greedy);
+  const double slope = a.slope(b, &greedy);
+  if (of_target && i == 0 && c == 0 && lane == 0) a.ticket[b] = 0;
   if (greedy && !of_target) return;
   const T* row = of_target ? a.target_row(b, i) : a.draft_row(b, i);
   const int base = c * kChunk - lead_of(row);
-  float x[J][VEC];
+  float x[kRowPer];
 #pragma unroll
   for (int j = 0; j < J; ++j) {
-    const int v = base + (j * kThreads + (int)threadIdx.x) * VEC;
+    const int v = base + (j * 64 + lane) * VEC;
     if (v >= 0 && v <= a.vocab - VEC) {
-      load_vec(row + v, x[j]);
+      load_vec(row + v, x + j * VEC);
     } else {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        x[j][e] = v + e >= 0 && v + e < a.vocab ? ld(row + v + e) : -INFINITY;
+        x[j * VEC + e] = v + e >= 0 && v + e < a.vocab ? ld(row + v + e) : -INFINITY;
     }
   }
   float top = -INFINITY;
-  int at = INT_MAX;
+  int at = 0;
+  double s = 0.0;
+  if (greedy) {
+    at = INT_MAX;
 #pragma unroll
-  for (int j = 0; j < J; ++j)
-#pragma unroll
-    for (int e = 0; e < VEC; ++e)
-      if (x[j][e] > top) {
-        top = x[j][e];
-        at = base + (j * kThreads + (int)threadIdx.x) * VEC + e;
+    for (int e = 0; e < kRowPer; ++e)
+      if (x[e] > top) {
+        top = x[e];
+        at = base + (e / VEC * 64 + lane) * VEC + e % VEC;
       }
-  for (int o = 32; o > 0; o >>= 1) {
-    const float ot = __shfl_xor(top, o, 64);
-    const int oa = __shfl_xor(at, o, 64);
-    if (ot > top || (ot == top && oa < at)) { top = ot; at = oa; }
-  }
-  if ((threadIdx.x & 63) == 0) {
-    tops[threadIdx.x >> 6] = top;
-    ats[threadIdx.x >> 6] = at;
-  }
-  __syncthreads();
-  top = tops[0];
-  at = ats[0];
-  for (int w = 1; w < kThreads / 64; ++w)
-    if (tops[w] > top || (tops[w] == top && ats[w] < at)) { top = tops[w]; at = ats[w]; }
-  double s = 0.0;
-  if (!greedy && at != INT_MAX) {
+    wave_first_max(top, at);
+  } else {
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int e = 0; e < kRowPer; ++e) top = fmaxf(top, x[e]);   // leaves NaN out
+    top = max_f32(top);
+    if (top > -INFINITY) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s += weight(x[j][e], top, inv);
+      for (int e = 0; e < kRowPer; ++e) s += weight(x[e], top, slope);
+      s = sum_f64(s);
+    }
   }
-  s = block_sum(s, sh);
-  if (threadIdx.x == 0) a.part[(int64_t)r * a.chunks + c] = Part{s, top, at};
+  if (lane == 0) a.part[(int64_t)r * a.chunks + c] = Part{s, top, at};
 }
 
-// A row's maximum, the first index of it, and its sum, by one wave.
-__device__ __forceinline__ Part row_total(const Part* part, int chunks, double inv) {
+// A row's maximum (greedy: with its first index) and its sum, by one wave.
+__device__ __forceinline__ Part row_total(const Part* part, int chunks, double slope, bool greedy) {
   const int lane = threadIdx.x & 63;
-  float top = -INFINITY;
-  int at = INT_MAX;
-  for (int c = lane; c < chunks; c += 64)
-    if (part[c].top > top) { top = part[c].top; at = part[c].at; }
-  for (int o = 32; o > 0; o >>= 1) {
-    const float ot = __shfl_xor(top, o, 64);
-    const int oa = __shfl_xor(at, o, 64);
-    if (ot > top || (ot == top && oa < at)) { top = ot; at = oa; }
+  Part own{0.0, -INFINITY, INT_MAX};
+  if (lane < chunks) own = part[lane];
+  if (greedy) {
+    for (int c = lane + 64; c < chunks; c += 64)
+      if (part[c].top > own.top) own = part[c];
+    wave_first_max(own.top, own.at);
+    return own;
   }
-  double s = 0.0;
-  for (int c = lane; c < chunks; c += 64) s += part[c].sum * weight(part[c].top, top, inv);
-  return Part{wave_sum_f64(s), top, at};
+  float top = own.top;
+  for (int c = lane + 64; c < chunks; c += 64) top = fmaxf(top, part[c].top);
+  top = max_f32(top);
+  if (!(top > -INFINITY)) return Part{0.0, top, INT_MAX};
+  double s = own.sum * weight(own.top, top, slope);
+  for (int c = lane + 64; c < chunks; c += 64) s += part[c].sum * weight(part[c].top, top, slope);
+  return Part{sum_f64(s), top, 0};
 }
 
-// The decision (by every workgroup of a sequence for itself: a few partials from L2
-// cost less than one more kernel), and the chunk's share of what the next token is
-// drawn from.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_decide_kernel(Verify<T> a) {
-  __shared__ double sh[kThreads / 64];
-  __shared__ int first;
-  const int b = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks;
-  const int wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
+  __shared__ double sh[kWaves];
+  __shared__ Part pt[kBlock], qt[kBlock];
+  __shared__ Part p_row;
+  __shared__ int first, firsts[kWaves], lasts[kWaves];
+  __shared__ bool is_last;
+  const int b = blockIdx.x / a.groups, group = blockIdx.x % a.groups;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = a.drafts(b);
   bool greedy;
-  const double inv = a.inverse(b, &greedy);
-  if (threadIdx.x == 0) first = n;
-  __syncthreads();
-  for (int i = wave; i < n; i += kThreads / 64) {
-    const Part p = row_total(a.target_part(b, i), a.chunks, inv);
-    const int x = a.tokens[(int64_t)b * a.g + i];
-    const bool in = x >= 0 && x < a.vocab;
-    bool keep;
-    if (greedy) {
-      keep = in && x == p.at;
-    } else {
-      double qx = a.draft ? 0.0 : 1.0;
-      if (a.draft && in) {
-        const Part q = row_total(a.draft_part(b, i), a.chunks, inv);
-        if (q.sum > 0.0) qx = weight(ld(a.draft_row(b, i) + x), q.top, inv) / q.sum;
-      }
-      const double px =
-          in && p.sum > 0.0 ? weight(ld(a.target_row(b, i) + x), p.top, inv) / p.sum : 0.0;
-      keep = (double)a.u[(int64_t)b * (a.g + 1) + i] * qx < px;
-    }
-    if (!keep && (threadIdx.x & 63) == 0) atomicMin(&first, i);
-  }
-  __syncthreads();
-  const int kept = first;
-  const Part p = row_total(a.target_part(b, kept), a.chunks, inv);
-  Part q{0.0, 0.0f, 0};
-  Pick k{};
-  k.kept = kept;
-  k.at = p.at;
-  k.mode = greedy ? kPickGreedy : kept == n ? kPickRow : a.draft ? kPickRest : kPickOthers;
-  if (k.mode == kPickRest) {
-    q = row_total(a.draft_part(b, kept), a.chunks, inv);
-    if (q.sum <= 0.0) k.mode = kPickRow;
-  }
-  if (k.mode == kPickOthers) k.gone = a.tokens[(int64_t)b * a.g + kept];
-  k.p_total = p.sum;
-  k.p_top = p.top;
-  k.q_total = q.sum;
-  k.q_top = q.top;
-  if (c == 0 && threadIdx.x == 0) a.pick[b] = k;
-  if (k.mode == kPickGreedy || !(p.sum > 0.0)) return;
-  const T* row = a.target_row(b, kept);
-  const Part own = a.target_part(b, kept)[c];
-  double s = own.sum * weight(own.top, p.top, inv);
-  const int lo = c * kChunk - (k.mode == kPickRest ? 0 : lead_of(row));
-  if (k.mode == kPickRest || (k.mode == kPickOthers && k.gone >= lo && k.gone < lo + kChunk)) {
-    const T* other = k.mode == kPickRest ? a.draft_row(b, kept) : row;
-    s = 0.0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int v = lo + j * kThreads + (int)threadIdx.x;
-      if (v < 0 || v >= a.vocab) continue;
-      const double w = weight(ld(row + v), p.top, inv);
-      if (k.mode == kPickRest)
-        s += fmax(w / p.sum - weight(ld(other + v), q.top, inv) / q.sum, 0.0);
-      else
-        s += v == k.gone ? 0.0 : w;
-    }
-    s = block_sum(s, sh);
-  }
-  if (threadIdx.x == 0) a.rest[(int64_t)b * a.chunks + c] = s;
-}
+  const double slope = a.slope(b, &greedy);
+  const float u_last = a.u[(int64_t)b * (a.g + 1) + a.g];
 
-// The next token of a sequence: the first index whose running sum passes u times the
-// whole.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_pick_kernel(Verify<T> a) {
-  __shared__ double sh[kThreads / 64];
-  __shared__ int found, last;
-  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Pick k = a.pick[b];
-  bool greedy;
-  const double inv = a.inverse(b, &greedy);
+  // the first draft that is not kept
+  int kept = n;
+  Part q{0.0, 0.0f, 0};
+  for (int i0 = 0; i0 < n; i0 += kBlock) {
+    const int m = min(n - i0, kBlock);
+    // wave 0, lane i: draft i0 + i
+    float lp = -INFINITY, lq = -INFINITY, u = 0.0f;
+    int x = -1;
+    if (tid < m) {
+      x = a.tokens[(int64_t)b * a.g + i0 + tid];
+      u = a.u[(int64_t)b * (a.g + 1) + i0 + tid];
+      if (x < 0 || x >= a.vocab) x = -1;
+      if (x >= 0 && !greedy) {
+        lp = ld(a.target_row(b, i0 + tid) + x);
+        if (a.draft) lq = ld(a.draft_row(b, i0 + tid) + x);
+      }
+    }
+    for (int i = wave; i < m; i += kWaves) {
+      const Part p = row_total(a.target_part(b, i0 + i), a.chunks, slope, greedy);
+      Part r{0.0, 0.0f, 0};
+      if (a.draft && !greedy) r = row_total(a.draft_part(b, i0 + i), a.chunks, slope, false);
+      if (lane == 0) {
+        pt[i] = p;
+        qt[i] = r;
+      }
+    }
+    __syncthreads();
+    if (wave == 0) {
+      bool keep = true;
+      if (lane < m) {
+        const Part p = pt[lane], r = qt[lane];
+        if (greedy) {
+          keep = x >= 0 && x == p.at;
+        } else {
+          const double px = x >= 0 && p.sum > 0.0 ? weight(lp, p.top, slope) / p.sum : 0.0;
+          const double qx = !a.draft ? 1.0
+                            : x >= 0 && r.sum > 0.0 ? weight(lq, r.top, slope) / r.sum : 0.0;
+          keep = (double)u * qx < px;
+        }
+      }
+      const uint64_t no = __ballot(!keep);
+      if (lane == 0) first = no ? __ffsll((unsigned long long)no) - 1 : m;
+    }
+    __syncthreads();
+    const int f = first;
+    if (f < m) {
+      kept = i0 + f;
+      q = qt[f];
+      if (tid == 0) p_row = pt[f];
+      break;
+    }
+    __syncthreads();
+  }
+  if (kept == n && wave == 0) {
+    const Part p = row_total(a.target_part(b, n), a.chunks, slope, greedy);
+    if (lane == 0) p_row = p;
+  }
+  __syncthreads();
+  const Part p = p_row;
+  int mode = greedy ? kPickGreedy : kept == n ? kPickRow : a.draft ? kPickRest : kPickOthers;
+  if (mode == kPickRest && !(q.sum > 0.0)) mode = kPickRow;
+  if (!greedy && !(p.sum > 0.0)) mode = kPickGreedy;   // no distribution: p.at is no token
+  if (mode != kPickRest && group != 0) return;
+
+  const T* row = a.target_row(b, kept);
+  const T* other = mode == kPickRest ? a.draft_row(b, kept) : row;
+  int gone = mode == kPickOthers ? a.tokens[(int64_t)b * a.g + kept] : -1;
+  const double ip = mode == kPickRest ? 1.0 / p.sum : 1.0, iq = mode == kPickRest ? 1.0 / q.sum : 0.0;
+  // what token v holds in this mode
+  auto held = [&](int v) {
+    if (v < 0 || v >= a.vocab || v == gone) return 0.0;
+    const double w = weight(ld(row + v), p.top, slope);
+    if (mode != kPickRest) return w;
+    // what is within the rounding of the rows' sums is none: of equal rows nothing is left
+    const double pv = w * ip, d = pv - weight(ld(other + v), q.top, slope) * iq;
+    return d > pv * 0x1p-40 ? d : 0.0;
+  };
+  if (mode == kPickRest) {
+    // The shares' sums meet by device-scope atomics, so no cache has to be written back in
+    // between; a workgroup counts itself once its atomics have returned, so the one that
+    // counts last finds every sum (with fences instead 84 us at 64 sequences).
+    uint64_t seen = 0;
+    for (int t = group; t < a.tiles; t += a.groups) {
+      double s = 0.0;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) s += held(t * kTile + j * kThreads + tid);
+      s = block_sum(s, sh);
+      if (tid == 0)
+        seen |= __hip_atomic_exchange(&a.rest[(int64_t)b * a.tiles + t], __builtin_bit_cast(uint64_t, s),
+                                      __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (tid == 0) {
+      unsigned one = 1;
+      asm volatile("" : "+v"(one) : "v"(seen));   // counted after the sums are there
+      is_last = __hip_atomic_fetch_add(&a.ticket[b], one, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT) == (unsigned)a.groups - 1;
+      asm volatile("" ::: "memory");
+    }
+    __syncthreads();
+    if (!is_last) return;
+  }
+
   int next = -1;
-  if (greedy) {
-    if (k.at != INT_MAX) next = k.at;
-  } else if (k.p_total > 0.0) {
-    const T* row = a.target_row(b, k.kept);
-    const Part* part = a.target_part(b, k.kept);
-    // every wave for itself, 64 chunks at a time
+  if (mode == kPickGreedy) {
+    if (greedy && p.at != INT_MAX) next = p.at;
+  } else {
+    // parts of the row that are searched: shares, or the first kernel's chunks
+    const Part* part = a.target_part(b, kept);
+    const int lead = lead_of(row);
+    double whole_gone = 0.0;              // kPickOthers: the chunk of the token left out
+    int c_gone = gone >= 0 && gone < a.vocab ? (gone + lead) / kChunk : -1;
+    if (c_gone >= 0) {
+      double s = 0.0;
+      for (int j = tid; j < kChunk; j += kThreads) s += held(c_gone * kChunk - lead + j);
+      whole_gone = block_sum(s, sh);
+    }
     auto mass = [&](int c) {
+      if (mode == kPickRest) {
+        if (c >= a.tiles) return 0.0;
+        return __builtin_bit_cast(double, __hip_atomic_load(&a.rest[(int64_t)b * a.tiles + c],
+                                                            __ATOMIC_RELAXED,
+                                                            __HIP_MEMORY_SCOPE_AGENT));
+      }
       if (c >= a.chunks) return 0.0;
-      return k.mode == kPickRow ? part[c].sum * weight(part[c].top, k.p_top, inv)
-                                : a.rest[(int64_t)b * a.chunks + c];
+      if (c == c_gone) return whole_gone;
+      return part[c].top > -INFINITY ? part[c].sum * weight(part[c].top, p.top, slope) : 0.0;
     };
+    int parts = mode == kPickRest ? a.tiles : a.chunks;
     auto whole = [&]() {
       double s = 0.0;
-      for (int c = lane; c < a.chunks; c += 64) s += mass(c);
-      return wave_sum_f64(s);
+      for (int c = lane; c < parts; c += 64) s += mass(c);
+      return sum_f64(s);
     };
     double total = whole();
-    if (k.mode != kPickRow && !(total > 0.0)) {   // p is q: nothing is left of it
-      k.mode = kPickRow;
-      total = whole();
+    if (mode != kPickRow && !(total > 0.0)) {   // p is q: nothing is left of it
+      mode = kPickRow;
+      parts = a.chunks;
+      gone = c_gone = -1;
+      total = p.sum;
     }
-    const double r = (double)a.u[(int64_t)b * (a.g + 1) + a.g];
-    const double aim = r > 0.0 ? r * total : 0.0;
-    double before = 0.0;        // the sum of the chunks before `chunk`
-    int chunk = -1;
-    double run = 0.0;
-    for (int c0 = 0; c0 < a.chunks; c0 += 64) {
+    const double aim = u_last > 0.0f ? (double)u_last * total : 0.0;
+    double run = 0.0, before = 0.0;       // before: the sum of the parts before `hit`
+    int found_part = -1;
+    for (int c0 = 0; c0 < parts; c0 += 64) {   // every wave for itself
       const double m = mass(c0 + lane);
-      double s = m;
-      for (int o = 1; o < 64; o <<= 1) {
-        const double t = __shfl_up(s, o, 64);
-        if (lane >= o) s += t;
-      }
-      // the chunk that passes the aim, else the last one that holds something
+      const double s = scan_f64(m);
+      // the part that passes the aim, else the last one that holds something
       const uint64_t over = __ballot(m > 0.0 && run + s > aim);
       const uint64_t some = __ballot(m > 0.0);
       const int hit = over ? __ffsll((unsigned long long)over) - 1
                            : some ? 63 - __clzll((long long)some) : -1;
       if (hit >= 0) {
-        chunk = c0 + hit;
-        before = run + __shfl(s - m, hit, 64);
+        found_part = c0 + hit;
+        before = run + lane_f64(s - m, hit);
       }
       if (over) break;
-      run += __shfl(s, 63, 64);
+      run += lane_f64(s, 63);
     }
-    if (threadIdx.x == 0) {
-      found = INT_MAX;
-      last = -1;
-    }
-    __syncthreads();
-    if (chunk >= 0) {
-      const int lo = chunk * kChunk - (k.mode == kPickRest ? 0 : lead_of(row)) +
-                     (int)threadIdx.x * kPer;
-      const T* other = k.mode == kPickRest ? a.draft_row(b, k.kept) : row;
+    if (found_part >= 0) {
+      const int size = mode == kPickRest ? kTile : kChunk;
+      const int lo = found_part * size - (mode == kPickRest ? 0 : lead);
       double w[kPer], s = 0.0;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
-        const int v = lo + e;
-        w[e] = 0.0;
-        if (v >= 0 && v < a.vocab) {
-          w[e] = weight(ld(row + v), k.p_top, inv);
-          if (k.mode == kPickRest)
-            w[e] = fmax(w[e] / k.p_total - weight(ld(other + v), k.q_top, inv) / k.q_total, 0.0);
-          else if (k.mode == kPickOthers && v == k.gone)
-            w[e] = 0.0;
-        }
+        const int j = tid * kPer + e;
+        w[e] = j < size ? held(lo + j) : 0.0;
         s += w[e];
       }
-      double scan = s;
-      for (int o = 1; o < 64; o <<= 1) {
-        const double t = __shfl_up(scan, o, 64);
-        if (lane >= o) scan += t;
-      }
+      const double scan = scan_f64(s);
+      __syncthreads();
       if (lane == 63) sh[wave] = scan;
       __syncthreads();
       double at = before + (scan - s);
       for (int v = 0; v < wave; ++v) at += sh[v];
+      int hit = INT_MAX, last = -1;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
         at += w[e];
         if (w[e] > 0.0) {
-          if (at > aim) atomicMin(&found, lo + e);
-          atomicMax(&last, lo + e);
+          if (at > aim) hit = min(hit, lo + tid * kPer + e);
+          last = lo + tid * kPer + e;
         }
       }
+      // indices ascend with the lanes
+      const uint64_t hits = __ballot(hit != INT_MAX), some = __ballot(last >= 0);
+      hit = hits ? __builtin_amdgcn_readlane(hit, __ffsll((unsigned long long)hits) - 1) : INT_MAX;
+      last = some ? __builtin_amdgcn_readlane(last, 63 - __clzll((long long)some)) : -1;
+      if (lane == 0) {
+        firsts[wave] = hit;
+        lasts[wave] = last;
+      }
+      __syncthreads();
+      for (int v = 0; v < kWaves; ++v) {
+        hit = min(hit, firsts[v]);
+        last = max(last, lasts[v]);
+      }
+      next = hit != INT_MAX ? hit : last;
     }
-    __syncthreads();
-    next = found != INT_MAX ? found : last;
   }
-  for (int i = threadIdx.x; i <= a.g; i += kThreads)
+  for (int i = tid; i <= a.g; i += kThreads)
     a.out[(int64_t)b * (a.g + 1) + i] =
-        i < k.kept ? a.tokens[(int64_t)b * a.g + i] : i == k.kept ? next : -1;
-  if (threadIdx.x == 0) a.kept[b] = k.kept;
+        i < kept ? a.tokens[(int64_t)b * a.g + i] : i == kept ? next : -1;
+  if (tid == 0) a.kept[b] = kept;
 }
 
 int chunks_of(int vocab) { return ceil_div((long)vocab + 7, kChunk); }   // 7: the largest lead
+int tiles_of(int vocab) { return ceil_div(vocab, kTile); }
 struct VerifyWs {
-  size_t part, rest, pick, total;
+  size_t rest, ticket, total;
 };
 VerifyWs verify_ws(int64_t n_seq, int64_t g, int vocab) {
   auto align = [](size_t x) { return (x + 255) / 256 * 256; };
-  const int64_t c = chunks_of(vocab);
   VerifyWs w{};
-  w.part = 0;
-  w.rest = align((size_t)(n_seq * (2 * g + 1) * c) * sizeof(Part));
-  w.pick = w.rest + align((size_t)(n_seq * c) * sizeof(double));
-  w.total = w.pick + align((size_t)n_seq * sizeof(Pick));
+  w.rest = align((size_t)(n_seq * (2 * g + 1) * chunks_of(vocab)) * sizeof(Part));
+  w.ticket = w.rest + align((size_t)(n_seq * tiles_of(vocab)) * sizeof(uint64_t));
+  w.total = w.ticket + align((size_t)n_seq * sizeof(unsigned));
   return w;
 }
 
@@ -421,16 +498,19 @@ template <typename T>
 adept_status verify_launch(Verify<T> a, void* workspace, hipStream_t s) {
   const VerifyWs w = verify_ws(a.n_seq, a.g, a.vocab);
   a.chunks = chunks_of(a.vocab);
-  a.part = (Part*)((char*)workspace + w.part);
-  a.rest = (double*)((char*)workspace + w.rest);
-  a.pick = (Pick*)((char*)workspace + w.pick);
+  a.tiles = tiles_of(a.vocab);
+  a.part = (Part*)workspace;
+  a.rest = (uint64_t*)((char*)workspace + w.rest);
+  a.ticket = (unsigned*)((char*)workspace + w.ticket);
   const int rows = a.n_seq * (a.g + 1) + (a.draft ? a.n_seq * a.g : 0);
-  ADEPT_LAUNCH(verify_rows_kernel<T>, dim3((unsigned)rows * a.chunks), dim3(kThreads), 0, s, a);
+  // one wave a workgroup while that spreads them over the chip's CUs
+  const int units = rows * a.chunks, waves = units >= 4096 ? kWaves : 1;
+  ADEPT_LAUNCH(verify_rows_kernel<T>, dim3(ceil_div(units, waves)), dim3(64 * waves), 0, s, a, rows);
   ADEPT_CHECK_LAUNCH("verify_rows");
-  ADEPT_LAUNCH(verify_decide_kernel<T>, dim3((unsigned)a.n_seq * a.chunks), dim3(kThreads), 0, s, a);
-  ADEPT_CHECK_LAUNCH("verify_decide");
-  ADEPT_LAUNCH(verify_pick_kernel<T>, dim3(a.n_seq), dim3(kThreads), 0, s, a);
-  return launch_status("verify_pick");
+  // shares only where something can be left of p - q; about 1024 workgroups at most
+  a.groups = a.draft ? std::min(a.tiles, std::max(1, 1024 / a.n_seq)) : 1;
+  ADEPT_LAUNCH(verify_token_kernel<T>, dim3((unsigned)a.n_seq * a.groups), dim3(kThreads), 0, s, a);
+  return launch_status("verify_token");
 }
 
 }  // namespace
