@@ -277,6 +277,7 @@ enum EpiKind {
 // A matrix in 4 bits (quant.h), and SWIGLU's second one.
 struct QuantView {
   const uint8_t *codes, *scales, *codes2, *scales2;
+  int row_blocks, col_blocks;   // of the launch (gemm_direct.hip)
 };
 
 struct GemmArgs {

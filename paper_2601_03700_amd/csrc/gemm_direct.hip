@@ -21,6 +21,9 @@
 // norms and row list 131 -> 102 (4.5 TB/s of weights in gate/up); width 1600,
 // 24 rows, QKV / first MLP 13.5 / 13.0 -> 11.0 / 10.3; width 768, 48 rows, biased
 // QKV 9.4 -> 6.8, in the skinny path's order (SPLIT) 8.0.
+#include <algorithm>
+#include <cmath>
+
 #include "gemm_tile.h"
 #include "quant.h"
 
@@ -74,11 +77,13 @@ __device__ __forceinline__ void store_any(const GP& p, int m, int n, const float
 // Q4: the weights in 4 bits (quant.h), in pieces of 128 of K: 16 bytes and four scale
 // bytes of a lane are its operands of four products.  v_cvt_scalef32_pk_bf16_fp4 makes
 // two bf16 of a byte, times the scale, exactly.  NB == 4 with a pair epilogue: two
-// blocks of the first kind, then their partners.
+// blocks of the first kind, then their partners.  A workgroup has 16 activation rows;
+// those of the other rows of the same weights run on the same XCD, whose L2 then has
+// them.  quant_form says which NB and W.
 template <int EPI, int NB, int MB, int W, int U, bool SPLIT, bool Q4>
 __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, int row_norm,
                                                              SkSplit sp, QuantView qv) {
-  static_assert(!(SPLIT && Q4) && (NB <= 2 || Q4), "forms");
+  static_assert(!(SPLIT && Q4) && (NB <= 2 || Q4) && (MB == 1 || !Q4), "forms");
   constexpr int KP = Q4 ? kQuantK : BK, HS = KP / 32;   // of K: a piece, products of one
   constexpr int HALF = NB == 4 ? 2 : 1;                 // blocks of one kind
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -89,6 +94,19 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, q = lane >> 4;
+  // Q4: the columns' workgroup and the first row
+  int bx = blockIdx.x, m0 = 0;
+  [[maybe_unused]] bool again = false;                  // the weights are read by others too
+  if constexpr (Q4) {
+    const int blocks = qv.row_blocks;
+    if (blocks > 1) {
+      const int i = bx >> 3;
+      m0 = i % blocks * 16;
+      bx = i / blocks * 8 + (bx & 7);
+      if (bx >= qv.col_blocks) return;
+      again = true;
+    }
+  }
   const int KT = Q4 ? (p.K + KP - 1) / KP : p.K / BK;
   const bool rope = EPI == EPI_QKV && p.rope_cos;
   const bool pair = EPI == EPI_SWIGLU || rope;
@@ -99,12 +117,10 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   if (rope) {
     dn = p.head_dim >> 1;
     const int cpb = dn / per;   // blocks per head
-    n0 = (int)blockIdx.x / cpb * p.head_dim + (int)blockIdx.x % cpb * per;
+    n0 = bx / cpb * p.head_dim + bx % cpb * per;
   } else {
-    n0 = blockIdx.x * (EPI == EPI_SWIGLU ? per : 16 * NB);
+    n0 = bx * (EPI == EPI_SWIGLU ? per : 16 * NB);
   }
-  // more than 64 rows (plain stores): 64 of them for each grid row
-  const int m0 = Q4 && EPI == EPI_STORE ? (int)blockIdx.y * kDirectRows : 0;
   // raw list entries: loaded before the row count is known, used below it
   int raw[MB];
 #pragma unroll
@@ -118,7 +134,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
 #pragma unroll
   for (int i = 0; i < G; ++i) {
     const int t = wave + W * i, y = t / XB;
-    pre[i].m = 16 * y + r16;
+    pre[i].m = m0 + 16 * y + r16;
     pre[i].row = kRows && !rl.exit_layer ? p.rows[min(pre[i].m, p.M_max - 1)] : 0;
   }
   int el = INT_MAX, act = 0;
@@ -164,8 +180,8 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
 #pragma unroll
       for (int x = 0; x < NB; ++x) {
         if constexpr (Q4) {
-          bw[st][u][x][0] = __builtin_nontemporal_load(
-              reinterpret_cast<const u32x4_t*>(br[x] + (int64_t)c * kQuantBlock));
+          const u32x4_t* w = reinterpret_cast<const u32x4_t*>(br[x] + (int64_t)c * kQuantBlock);
+          bw[st][u][x][0] = again ? *w : __builtin_nontemporal_load(w);
           sw[st][u][x] = *reinterpret_cast<const uint32_t*>(sr[x] + (int64_t)c * kQuantScales);
         } else {
 #pragma unroll
@@ -185,7 +201,6 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   // the rows: active rows, then (row list) the rows that exited before the
   // layer, in one ballot of at most 64 token rows
   int M = p.M_dev ? min(*p.M_dev, rl.exit_layer ? rl.max_act : p.M_max) : p.M_max;
-  if constexpr (Q4 && EPI == EPI_STORE) M = min(M - m0, kDirectRows);
   if (rl.ticket && blockIdx.x == 0 && threadIdx.x < 2) rl.ticket[threadIdx.x] = 0ull;
   const bf16* ar[MB];
   if (rl.exit_layer) {
@@ -205,20 +220,20 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
       }
     }
     __syncthreads();
-    if (M <= 0) return;
+    if (M <= m0) return;
 #pragma unroll
     for (int y = 0; y < MB; ++y) {
-      const int m = min(16 * y + r16, M - 1);
+      const int m = min(m0 + 16 * y + r16, M - 1);
       ar[y] = (from2[m] ? p.A2 : p.A) + (int64_t)list[m] * p.lda + 8 * q;
     }
 #pragma unroll
     for (int i = 0; i < G; ++i) pre[i].row = list[min(pre[i].m, M - 1)];
   } else {
-    if (M <= 0) return;
+    if (M <= m0) return;
 #pragma unroll
     for (int y = 0; y < MB; ++y) {
       // rows past the count: row 0, computed and never stored
-      const int row = 16 * y + r16 < M ? raw[y] : 0;
+      const int row = m0 + 16 * y + r16 < M ? raw[y] : 0;
       ar[y] = ((p.a_sel && (p.a_sel[row] & 1)) ? p.A2 : p.A) + (int64_t)row * p.lda + 8 * q;
     }
 #pragma unroll
@@ -232,7 +247,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
       if (c >= hi) continue;
 #pragma unroll
       for (int y = 0; y < MB; ++y)
-        if (y == 0 || 16 * y < M) {
+        if (y == 0 || 16 * y < M) {   // (Q4: one block)
 #pragma unroll
           for (int h = 0; h < HS; ++h) {
             if constexpr (Q4) {
@@ -240,7 +255,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
               // are too, but not what memory holds: 0 times NaN); a lane without a row
               // loads nothing
               aw[st][u][y][h] = u32x4_t{0, 0, 0, 0};
-              if (16 * y + r16 < M && c * KP + 32 * h + 8 * q < p.K)
+              if (m0 + r16 < M && c * KP + 32 * h + 8 * q < p.K)
                 aw[st][u][y][h] =
                     *reinterpret_cast<const u32x4_t*>(ar[y] + (int64_t)c * KP + 32 * h);
             } else {
@@ -436,7 +451,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
     if (row_norm) {
       float s = 0.0f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) s += ssq[w][e.m];
+      for (int w = 0; w < W; ++w) s += ssq[w][e.m - m0];
       sc = 1.0f / sqrtf(s / (float)p.K + p.row_eps);
     }
     const float4 x4 = sum(y * NB + x, lane);
@@ -445,7 +460,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
     bf16x4_t o;
     if constexpr (EPI == EPI_STORE) {
       if constexpr (Q4) {
-        store_any(p, m0 + e.m, e.n, v);
+        store_any(p, e.m, e.n, v);
         continue;
       }
       if (p.c_f32) {
@@ -499,7 +514,7 @@ int split_segments(const SkSplit& sp) {
 
 template <int EPI, int NB, int MB, int W, int U, bool SPLIT, bool Q4 = false>
 adept_status dir_launch(const GP& p, const RowList& rl, int row_norm, const char* name,
-                        hipStream_t s, const QuantView& qv = QuantView{}) {
+                        hipStream_t s, QuantView qv = QuantView{}) {
   SkSplit sp{};
   int parts = W;
   if (SPLIT) {
@@ -512,11 +527,15 @@ adept_status dir_launch(const GP& p, const RowList& rl, int row_norm, const char
     ADEPT_TRY(lds_limit((const void*)gemm_direct_kernel<EPI, NB, MB, W, U, SPLIT, Q4>,
                         SPLIT ? kSplitLds : red, &attr_set, "gemm_direct LDS limit"));
   const int cols = EPI == EPI_SWIGLU ? 8 * NB : 16 * NB;
-  const dim3 grid(ceil_div(p.N, cols),
-                  Q4 && EPI == EPI_STORE ? ceil_div(p.M_max, kDirectRows) : 1);
+  int grid = ceil_div(p.N, cols);
+  if (Q4) {
+    qv.col_blocks = grid;
+    qv.row_blocks = ceil_div(rl.exit_layer ? rl.n_tok : p.M_max, 16);
+    if (qv.row_blocks > 1) grid = ceil_div(grid, 8) * 8 * qv.row_blocks;
+  }
   {
     TimedLaunch tl(name ? name : "gemm_direct", s);
-    hipLaunchKernelGGL((gemm_direct_kernel<EPI, NB, MB, W, U, SPLIT, Q4>), grid, dim3(64 * W), red,
+    hipLaunchKernelGGL((gemm_direct_kernel<EPI, NB, MB, W, U, SPLIT, Q4>), dim3(grid), dim3(64 * W), red,
                        s, p, rl, row_norm, sp, qv);
   }
   return launch_status("gemm_direct");
@@ -548,18 +567,43 @@ adept_status dir_rows(const GP& p, const RowList& rl, int row_norm, const char* 
               : dir_launch<EPI, 1, 4, 8, SPLIT ? 2 : 1, SPLIT>(p, rl, row_norm, name, s);
 }
 
-// Weights in 4 bits.
+// Weights in 4 bits: NB blocks of 16 weight rows, W waves.  The form with the least
+// of an estimate of a CU's time: the loads of its workgroups' waves (a piece of K:
+// the activations', which lanes without a row leave out, and one for each block),
+// their fixed part, and the rounds of pieces that wait for each other.  The weights of
+// the three are fitted to the times of these four forms, of W = 4 .. 16 with NB = 1 .. 4
+// at 1 to 64 rows, n 320 .. 50304 and k 512 .. 11008 (266 shapes): the choice is 2.7 %
+// behind the best of all on average and 22 % at most.  A rule on n alone (NB = 1 below
+// 16384 columns) was 82 % behind at 16 rows of 11008 x 11008: 35.6 us, 19.6 with NB = 4.
+struct QuantForm { int nb, w; };
+QuantForm quant_form(int rows, int n_weights, int K) {
+  static const QuantForm forms[] = {{1, 16}, {2, 16}, {4, 8}, {4, 4}};
+  const int pieces = ceil_div(K, kQuantK);
+  const double x = 0.25 + 1.2 * std::min(rows, 16) / 16;
+  QuantForm best{};
+  double least = 0;
+  for (const QuantForm& f : forms) {
+    const double wgs = ceil_div((long)ceil_div(n_weights, 16 * f.nb) * ceil_div(rows, 16), 256);
+    const int rounds = ceil_div(pieces, f.w);
+    const double t = wgs * f.w * (rounds * (x + 0.65 * f.nb) + 2.4) +
+                     9.0 * rounds * std::ceil(wgs * f.w / 16);
+    if (best.nb == 0 || t < least) {
+      best = f;
+      least = t;
+    }
+  }
+  return best;
+}
+
 template <int EPI>
 adept_status quant_rows(const GP& p, const RowList& rl, int row_norm, const QuantView& qv,
                         const char* name, hipStream_t s) {
-  const int M = rl.exit_layer ? rl.n_tok : p.M_max;
-  const int tiles = ceil_div(EPI == EPI_SWIGLU ? 2 * p.N : p.N, 16);
-  if (M <= 16) return dir_launch<EPI, 1, 1, 8, 2, false, true>(p, rl, row_norm, name, s, qv);
-  if (M <= 32)
-    return tiles >= 512 ? dir_launch<EPI, 2, 2, 8, 1, false, true>(p, rl, row_norm, name, s, qv)
-                        : dir_launch<EPI, 1, 2, 8, 1, false, true>(p, rl, row_norm, name, s, qv);
-  return tiles >= 512 ? dir_launch<EPI, 2, 4, 8, 1, false, true>(p, rl, row_norm, name, s, qv)
-                      : dir_launch<EPI, 1, 4, 8, 1, false, true>(p, rl, row_norm, name, s, qv);
+  const QuantForm f = quant_form(rl.exit_layer ? rl.n_tok : p.M_max,
+                                 EPI == EPI_SWIGLU ? 2 * p.N : p.N, p.K);
+  if (f.nb == 1) return dir_launch<EPI, 1, 1, 16, 1, false, true>(p, rl, row_norm, name, s, qv);
+  if (f.nb == 2) return dir_launch<EPI, 2, 1, 16, 1, false, true>(p, rl, row_norm, name, s, qv);
+  if (f.w == 8) return dir_launch<EPI, 4, 1, 8, 1, false, true>(p, rl, row_norm, name, s, qv);
+  return dir_launch<EPI, 4, 1, 4, 1, false, true>(p, rl, row_norm, name, s, qv);
 }
 
 }  // namespace

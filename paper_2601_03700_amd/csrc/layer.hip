@@ -475,7 +475,7 @@ adept_status layer_step(const adept_layer_args* a, int layer, const PagedStep* p
   };
   auto quant_of = [&](GemmArgs& x, const adept_quant_mat& m, const adept_quant_mat* m2) {
     const adept_quant_mat p1 = packed(m, x.N, x.K);
-    x.quant = QuantView{(const uint8_t*)p1.codes, (const uint8_t*)p1.scales, nullptr, nullptr};
+    x.quant = QuantView{(const uint8_t*)p1.codes, (const uint8_t*)p1.scales, nullptr, nullptr, 0, 0};
     if (!m2) return;
     const adept_quant_mat p2 = packed(*m2, x.N, x.K);
     x.quant.codes2 = (const uint8_t*)p2.codes;

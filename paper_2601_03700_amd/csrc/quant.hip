@@ -186,7 +186,10 @@ extern "C" adept_status adept_quant_linear(int n, int k, const void* x, int64_t 
   ADEPT_REQUIRE(out_dt == ADEPT_F32 || out_dt == ADEPT_BF16, "quant_linear: bad dtype");
   ADEPT_TRY(check_matrix("quant_linear", n, k, codes, scales));
   ADEPT_REQUIRE(k % 8 == 0, "quant_linear: k = %d is no multiple of 8", k);
-  ADEPT_REQUIRE(max_rows >= 0 && max_rows <= 64 * 65535, "quant_linear: bad max_rows %d", max_rows);
+  // a grid's bound: workgroups of up to 1024 threads
+  ADEPT_REQUIRE(max_rows >= 0 && max_rows <= 64 * 65535 &&
+                    (ceil_div(n, 16) + 7ll) * ceil_div(max_rows, 16) < 1 << 22,
+                "quant_linear: bad max_rows %d", max_rows);
   if (max_rows == 0) return ADEPT_OK;
   ADEPT_REQUIRE(x && y && aligned16(x) && x_stride >= k && x_stride % 8 == 0,
                 "quant_linear: x must be 16-byte aligned rows, a multiple of 16 bytes apart");
@@ -197,7 +200,7 @@ extern "C" adept_status adept_quant_linear(int n, int k, const void* x, int64_t 
   g.M_max = max_rows; g.M_dev = n_rows; g.N = n; g.K = k;
   g.A = x; g.a_rows = rows; g.lda = x_stride; g.epi = EPI_STORE;
   g.C = y; g.ldc = y_stride; g.c_f32 = out_dt == ADEPT_F32; g.bias = bias; g.name = "quant_linear";
-  g.quant = QuantView{(const uint8_t*)codes, (const uint8_t*)scales, nullptr, nullptr};
+  g.quant = QuantView{(const uint8_t*)codes, (const uint8_t*)scales, nullptr, nullptr, 0, 0};
   return gemm_direct(g, as_stream(stream));
 }
 

@@ -62,7 +62,7 @@ def linear(n=20, k=40, x=A, xs=40, rows=None, n_rows=None, m=3, codes=A, scales=
 
 
 @pytest.mark.parametrize("bad", [dict(n=0), dict(k=0), dict(k=44, xs=48), dict(x=None), dict(x=A + 8),
-                                 dict(xs=32), dict(xs=44), dict(m=-1), dict(m=64 * 65536),
+                                 dict(xs=32), dict(xs=44), dict(m=-1), dict(m=64 * 65536), dict(n=32000, ys=32000, m=33600),
                                  dict(codes=None), dict(scales=A + 8), dict(bias=A + 1), dict(dt=2),
                                  dict(y=None), dict(ys=19), dict(y=A + 2),
                                  dict(dt=B.BF16, y=A + 1)], ids=str)
