@@ -83,7 +83,7 @@ __device__ __forceinline__ void store_any(const GP& p, int m, int n, const float
 template <int EPI, int NB, int MB, int W, int U, bool SPLIT, bool Q4>
 __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, int row_norm,
                                                              SkSplit sp, QuantView qv) {
-  static_assert(!(SPLIT && Q4) && (NB <= 2 || Q4) && (MB == 1 || !Q4), "forms");
+  static_assert(!(SPLIT && Q4) && (NB <= 2 || Q4) && (!Q4 || (MB == 1 && U == 1)), "forms");
   constexpr int KP = Q4 ? kQuantK : BK, HS = KP / 32;   // of K: a piece, products of one
   constexpr int HALF = NB == 4 ? 2 : 1;                 // blocks of one kind
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
     }
   }
   constexpr int BH = Q4 ? 1 : HS;                       // loads of a weight piece
-  u32x4_t bw[2][U][NB][BH], aw[2][U][MB][HS];
+  u32x4_t bw[2][U][NB][BH], aw[2][Q4 ? 1 : U][MB][HS];
   [[maybe_unused]] uint32_t sw[2][U][NB];
   // a stage: up to U pieces of K from c0 on, below hi
   constexpr int kStep = SPLIT ? 1 : W;
@@ -250,24 +250,50 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
         if (y == 0 || 16 * y < M) {   // (Q4: one block)
 #pragma unroll
           for (int h = 0; h < HS; ++h) {
-            if constexpr (Q4) {
-              // rows that are not there and K behind the last are zeros (the codes there
-              // are too, but not what memory holds: 0 times NaN); a lane without a row
-              // loads nothing
-              aw[st][u][y][h] = u32x4_t{0, 0, 0, 0};
-              if (m0 + r16 < M && c * KP + 32 * h + 8 * q < p.K)
-                aw[st][u][y][h] =
-                    *reinterpret_cast<const u32x4_t*>(ar[y] + (int64_t)c * KP + 32 * h);
-            } else {
-              aw[st][u][y][h] = *reinterpret_cast<const u32x4_t*>(ar[y] + (int64_t)c * KP + 32 * h);
-            }
+            aw[st][u][y][h] = *reinterpret_cast<const u32x4_t*>(ar[y] + (int64_t)c * KP + 32 * h);
           }
         }
     }
   };
+  // Q4: the activations of a round of pieces (one for each wave) go through LDS, where a
+  // wave brings 16 / W rows of them in 1 KiB loads: straight from global memory to the
+  // operands, 64 bytes of 16 rows a load, 16 rows of 4096 x 11008 took 14.2 us, XXX so.
+  constexpr int kSeg = W * 256, kXRow = kSeg + 16;      // bytes of a row in a round, in LDS
+  constexpr int kRowsW = 16 / W < 1 ? 1 : 16 / W, kLoads = 4 / kRowsW < 1 ? 1 : 4 / kRowsW;
+  [[maybe_unused]] u32x4_t xw[4];
+  [[maybe_unused]] const char* xr[kRowsW];
+  [[maybe_unused]] auto load_x = [&](int round) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = i / kLoads;
+      const int64_t at = (int64_t)round * kSeg + i % kLoads * 1024 + lane * 16;
+      // rows that are not there and K behind the last are zeros: the codes there are
+      // too, but 0 times what memory holds might be NaN
+      xw[i] = u32x4_t{0, 0, 0, 0};
+      if (m0 + kRowsW * wave + j < M && at < 2 * (int64_t)p.K)
+        xw[i] = *reinterpret_cast<const u32x4_t*>(xr[j] + at);
+    }
+  };
+  [[maybe_unused]] auto store_x = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<u32x4_t*>(smem + (buf * 16 + kRowsW * wave + i / kLoads) * kXRow +
+                                  i % kLoads * 1024 + lane * 16) = xw[i];
+  };
+  if constexpr (Q4) {
+    // a lane's row pointer from the lane that has it
+    const uint64_t own = (uint64_t)(uintptr_t)(ar[0] - 8 * q);
+#pragma unroll
+    for (int j = 0; j < kRowsW; ++j) {
+      const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)own, kRowsW * wave + j);
+      const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(own >> 32), kRowsW * wave + j);
+      xr[j] = (const char*)(uintptr_t)((uint64_t)hi << 32 | lo);
+    }
+    load_x(0);
+  }
   if constexpr (SPLIT) {
     if (wave < nseg) load_a(lo_of(wave), hi_of(wave), 0);
-  } else {
+  } else if constexpr (!Q4) {
     load_a(wave, KT, 0);
   }
   // the epilogue's inputs
@@ -328,7 +354,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
 #pragma unroll
         for (int y = 0; y < MB; ++y)
           if (y == 0 || 16 * y < M) {
-            const u32x4_t a = aw[st][u][y][h];
+            const u32x4_t a = aw[Q4 ? 0 : st][Q4 ? 0 : u][y][h];
 #pragma unroll
             for (int x = 0; x < NB; ++x)
               acc[y][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
@@ -395,6 +421,37 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
       s = s1;
       c = c1;
     }
+  } else if constexpr (Q4) {
+    const int rounds = (KT + W - 1) / W;
+    auto piece = [&](int round, int st) {
+      if (round * W + wave >= KT) return;
+      const char* xb = smem + ((round & 1) * 16 + r16) * kXRow + wave * 256 + q * 16;
+#pragma unroll
+      for (int h = 0; h < HS; ++h) aw[0][0][0][h] = *reinterpret_cast<const u32x4_t*>(xb + 64 * h);
+      step(round * W + wave, KT, st);
+    };
+    store_x(0);
+#pragma unroll 1
+    for (int r = 0; r < rounds; r += 2) {
+      if (r + 1 < rounds) {
+        load_x(r + 1);
+        load_b((r + 1) * W + wave, KT, 1);
+      }
+      __syncthreads();
+      piece(r, 0);
+      if (r + 1 < rounds) {
+        store_x(1);
+        if (r + 2 < rounds) {
+          load_x(r + 2);
+          load_b((r + 2) * W + wave, KT, 0);
+        }
+        __syncthreads();
+        piece(r + 1, 1);
+        if (r + 2 < rounds) store_x(0);
+      }
+    }
+    __syncthreads();   // the sums take the activations' place
+    hand_over(wave);
   } else {
     const int mine = KT > wave ? (KT - wave + W - 1) / W : 0;   // this wave's pieces of K
     const int iters = (mine + U - 1) / U;
@@ -521,7 +578,8 @@ adept_status dir_launch(const GP& p, const RowList& rl, int row_norm, const char
     sp = skinny_split(p.N, p.K);
     parts = split_segments(sp);
   }
-  const size_t red = (size_t)parts * MB * NB * 1024;
+  const size_t sums = (size_t)parts * MB * NB * 1024;
+  const size_t red = Q4 ? std::max<size_t>(sums, 2 * 16 * (W * 256 + 16)) : sums;   // see kXRow
   static bool attr_set = false;
   if (SPLIT || red > 48 * 1024)
     ADEPT_TRY(lds_limit((const void*)gemm_direct_kernel<EPI, NB, MB, W, U, SPLIT, Q4>,
