@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   };
   // Q4: the activations of a round of pieces (one for each wave) go through LDS, where a
   // wave brings 16 / W rows of them in 1 KiB loads: straight from global memory to the
-  // operands, 64 bytes of 16 rows a load, 16 rows of 4096 x 11008 took 14.2 us, XXX so.
+  // operands, 64 bytes of 16 rows a load, 16 rows of 4096 x 11008 took 14.2 us, 9.8 so.
   constexpr int kSeg = W * 256, kXRow = kSeg + 16;      // bytes of a row in a round, in LDS
   constexpr int kRowsW = 16 / W < 1 ? 1 : 16 / W, kLoads = 4 / kRowsW < 1 ? 1 : 4 / kRowsW;
   [[maybe_unused]] u32x4_t xw[4];
@@ -625,26 +625,28 @@ adept_status dir_rows(const GP& p, const RowList& rl, int row_norm, const char* 
               : dir_launch<EPI, 1, 4, 8, SPLIT ? 2 : 1, SPLIT>(p, rl, row_norm, name, s);
 }
 
-// Weights in 4 bits: NB blocks of 16 weight rows, W waves.  The form with the least
-// of an estimate of a CU's time: the loads of its workgroups' waves (a piece of K:
-// the activations', which lanes without a row leave out, and one for each block),
-// their fixed part, and the rounds of pieces that wait for each other.  The weights of
-// the three are fitted to the times of these four forms, of W = 4 .. 16 with NB = 1 .. 4
-// at 1 to 64 rows, n 320 .. 50304 and k 512 .. 11008 (266 shapes): the choice is 2.7 %
-// behind the best of all on average and 22 % at most.  A rule on n alone (NB = 1 below
-// 16384 columns) was 82 % behind at 16 rows of 11008 x 11008: 35.6 us, 19.6 with NB = 4.
+// Weights in 4 bits: NB blocks of 16 weight rows, W waves.  The form with the least of
+// an estimate of a CU's time, from its share of the workgroups: what their waves do a
+// piece (the activations' part grows with the rows, the weights' with NB), their fixed
+// part, and the rounds of pieces that wait for each other, of up to 16 waves at a time.
+// The weights of the four are fitted to the times of 315 shapes (1 to 64 rows, n 320 ..
+// 50304, k 512 .. 11008) in all of NB = 1, 2, 4 and W = 4, 8, 16: the choice is 1.5 %
+// behind the best on average and 11 % at most.  No form serves all: 16 rows of
+// 4096 x 11008 11.0 us with 1 x 16 and 16.0 with 4 x 16, 64 rows of 11008 x 4096 16.0
+// with 4 x 4 and 21.2 with 2 x 8, 1 row of 22016 x 4096 11.9 with 2 x 4 and 15.8 with
+// 1 x 4.  More activation rows of a workgroup (32, 64) convert the weights less often,
+// but few of them fit a CU: 64 rows of 11008 x 4096 18.6 us.
 struct QuantForm { int nb, w; };
 QuantForm quant_form(int rows, int n_weights, int K) {
-  static const QuantForm forms[] = {{1, 16}, {2, 16}, {4, 8}, {4, 4}};
+  static const QuantForm forms[] = {{1, 16}, {2, 16}, {2, 8}, {2, 4}, {4, 4}};
   const int pieces = ceil_div(K, kQuantK);
-  const double x = 0.25 + 1.2 * std::min(rows, 16) / 16;
   QuantForm best{};
   double least = 0;
   for (const QuantForm& f : forms) {
     const double wgs = ceil_div((long)ceil_div(n_weights, 16 * f.nb) * ceil_div(rows, 16), 256);
     const int rounds = ceil_div(pieces, f.w);
-    const double t = wgs * f.w * (rounds * (x + 0.65 * f.nb) + 2.4) +
-                     9.0 * rounds * std::ceil(wgs * f.w / 16);
+    const double t = wgs * f.w * (rounds * (0.33 * std::min(rows, 16) / 16 + 1.6 * f.nb) + 2.6) +
+                     20.0 * rounds * std::ceil(wgs * f.w / 16);
     if (best.nb == 0 || t < least) {
       best = f;
       least = t;
@@ -659,8 +661,11 @@ adept_status quant_rows(const GP& p, const RowList& rl, int row_norm, const Quan
   const QuantForm f = quant_form(rl.exit_layer ? rl.n_tok : p.M_max,
                                  EPI == EPI_SWIGLU ? 2 * p.N : p.N, p.K);
   if (f.nb == 1) return dir_launch<EPI, 1, 1, 16, 1, false, true>(p, rl, row_norm, name, s, qv);
-  if (f.nb == 2) return dir_launch<EPI, 2, 1, 16, 1, false, true>(p, rl, row_norm, name, s, qv);
-  if (f.w == 8) return dir_launch<EPI, 4, 1, 8, 1, false, true>(p, rl, row_norm, name, s, qv);
+  if (f.nb == 2 && f.w == 16)
+    return dir_launch<EPI, 2, 1, 16, 1, false, true>(p, rl, row_norm, name, s, qv);
+  if (f.nb == 2 && f.w == 8)
+    return dir_launch<EPI, 2, 1, 8, 1, false, true>(p, rl, row_norm, name, s, qv);
+  if (f.nb == 2) return dir_launch<EPI, 2, 1, 4, 1, false, true>(p, rl, row_norm, name, s, qv);
   return dir_launch<EPI, 4, 1, 4, 1, false, true>(p, rl, row_norm, name, s, qv);
 }
 

@@ -1,10 +1,9 @@
 // Weights in 4 bits (quant.h): packed from a matrix, read back, and the product of
 // few rows with them (the few-row GEMM of gemm_direct.hip over the packed form).
 //
-// Packing and reading back: one wave for a block of 16 rows and 128 of K; a lane has
-// the row and the eight k that its bytes in the block stand for, so that the codes are
-// written as 1 KiB at once and a group's largest magnitude is in four lanes.  Bound by
-// the HBM traffic of the source.
+// Packing and reading back: one wave for a block of 16 rows and 128 of K.  Packing
+// reads whole lines of the rows and turns the codes in LDS into the block's order.
+// Bound by the HBM traffic of the source.
 #include <climits>
 
 #include "quant.h"
@@ -45,48 +44,56 @@ __global__ __launch_bounds__(64 * kWaves) void quant_pack_kernel(int n, int k, c
                                                                  int64_t ldw, int kb, int64_t blocks,
                                                                  uint8_t* __restrict__ codes,
                                                                  uint8_t* __restrict__ scales) {
-  const int64_t blk = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  __shared__ __attribute__((aligned(16))) uint32_t turn[kWaves][kQuantBlock / 4];
+  __shared__ __attribute__((aligned(4))) uint8_t bytes[kWaves][kQuantScales];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t blk = (int64_t)blockIdx.x * kWaves + wave;
+  if (blk < blocks) {
+    const int64_t row0 = blk / kb * kQuantRows;
+    // a lane has eight of the 128 k of rows lane / 16 + 4 i, a group is four lanes
+    const int chunk = lane & 15, k0 = (int)(blk % kb) * kQuantK + 8 * chunk;
+    float x[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t row = row0 + 4 * i + (lane >> 4);
+      const int left = row < n ? min(max(k - k0, 0), 8) : 0;
+      const T* p = w + (left > 0 ? row * ldw + k0 : 0);
+      load8(p, left == 8 && ((uintptr_t)p & 15) == 0, left, x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[i][e]) & 0x7fffffffu);
+      top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+      // top = m 2^x, 1 <= m < 2: the least E with top <= 7 2^E = 1.75 2^(E + 2)
+      int b = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+      b = min(max(b, kQuantScaleMin), kQuantScaleMax);
+      const float inv = __uint_as_float((uint32_t)(254 - b) << 23);
+      const bool fine = top < 0x7f800000u;
+      if (!fine) b = kQuantScaleNan;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = fine ? x[i][e] * inv : 0.0f;   // exact, or far below 1/4
+      // to the nearest code, ties to even, at most 6
+      uint32_t c = 0;
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[0], y[1], 1.0f, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[2], y[3], 1.0f, 1);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[4], y[5], 1.0f, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[6], y[7], 1.0f, 3);
+      const int r16 = 4 * i + (lane >> 4), h = chunk >> 2, q = chunk & 3;
+      turn[wave][(r16 + 16 * q) * 4 + h] = c;
+      if (q == 0) bytes[wave][r16 * 4 + h] = (uint8_t)b;
+    }
+  }
+  __syncthreads();
   if (blk >= blocks) return;
-  const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
-  const int64_t row = blk / kb * kQuantRows + r16;
-  const int k0 = (int)(blk % kb) * kQuantK + 8 * q;
-  const T* src = w + row * ldw;
-  float x[4][8];
-#pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    const int left = row < n ? min(max(k - k0 - 32 * h, 0), 8) : 0;
-    const T* p = src + k0 + 32 * h;
-    load8(left > 0 ? p : w, left == 8 && ((uintptr_t)p & 15) == 0, left, x[h]);
-  }
-  uint32_t word[4], bytes = 0;
-#pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[h][e]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-    // top = m 2^x, 1 <= m < 2: the least E with top <= 7 2^E = 1.75 2^(E + 2)
-    int b = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-    b = min(max(b, kQuantScaleMin), kQuantScaleMax);
-    const float inv = __uint_as_float((uint32_t)(254 - b) << 23);
-    const bool fine = top < 0x7f800000u;
-    if (!fine) b = kQuantScaleNan;
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = fine ? x[h][e] * inv : 0.0f;   // exact, or far below 1/4
-    // to the nearest code, ties to even, at most 6
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[0], y[1], 1.0f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[2], y[3], 1.0f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[4], y[5], 1.0f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[6], y[7], 1.0f, 3);
-    word[h] = c;
-    bytes |= (uint32_t)b << (8 * h);
-  }
   *reinterpret_cast<uint4*>(codes + blk * kQuantBlock + lane * 16) =
-      make_uint4(word[0], word[1], word[2], word[3]);
-  if (q == 0) *reinterpret_cast<uint32_t*>(scales + blk * kQuantScales + r16 * 4) = bytes;
+      *reinterpret_cast<const uint4*>(&turn[wave][lane * 4]);
+  if (lane < kQuantScales / 4)
+    *reinterpret_cast<uint32_t*>(scales + blk * kQuantScales + lane * 4) =
+        *reinterpret_cast<const uint32_t*>(&bytes[wave][lane * 4]);
 }
 
 template <typename T>
