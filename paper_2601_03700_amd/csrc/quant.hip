@@ -13,11 +13,16 @@ namespace {
 
 constexpr int kWaves = 4;
 
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
 __device__ __forceinline__ void load8(const float* p, bool whole, int left, float (&x)[8]) {
   if (whole) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      const u32x4_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + i));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i + e] = __uint_as_float(w[e]);
+    }
     return;
   }
 #pragma unroll
@@ -25,8 +30,7 @@ __device__ __forceinline__ void load8(const float* p, bool whole, int left, floa
 }
 __device__ __forceinline__ void load8(const bf16* p, bool whole, int left, float (&x)[8]) {
   if (whole) {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    const u32x4_t u = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       x[2 * e] = __uint_as_float(u[e] << 16);
