@@ -85,29 +85,38 @@ __device__ __forceinline__ int lead_of(const T* row) {
 }
 
 // 2^x for x <= 0, 0 for NaN: 2^n 2^f with n = rint(x), and 2^f by the polynomial of
-// degree 10 through the Chebyshev points of [-1/2, 1/2] (off by 3e-16 of it).
-__device__ __forceinline__ double exp2_neg(double x) {
-  x = fmax(x, -1100.0);   // 2^-1100 is 0
-  const double n = rint(x), f = x - n;
-  double s = 7.072585949269223e-09;
-  s = fma(s, f, 1.0208690299958306e-07);
-  s = fma(s, f, 1.321544258792169e-06);
-  s = fma(s, f, 1.5252657260200837e-05);
-  s = fma(s, f, 0.0001540353044173605);
-  s = fma(s, f, 0.0013333558230164974);
-  s = fma(s, f, 0.009618129107606888);
-  s = fma(s, f, 0.05550410866444772);
-  s = fma(s, f, 0.24022650695910097);
-  s = fma(s, f, 0.69314718055995);
-  s = fma(s, f, 1.0);
-  return ldexp(s, (int)n);
-}
+// degree 10 through the Chebyshev points of [-1/2, 1/2] (off by 3e-16 of it).  The
+// first kernel is bound by these instructions: the coefficients are kept in scalar
+// registers (as constants they took two moves for each product, 640 instructions a
+// wave where XXX do).
+struct Exp2 {
+  double c[10];
+  __device__ __forceinline__ Exp2() {
+    constexpr double k[10] = {0.69314718055995,      0.24022650695910097,   0.05550410866444772,
+                              0.009618129107606888,  0.0013333558230164974, 0.0001540353044173605,
+                              1.5252657260200837e-05, 1.321544258792169e-06, 1.0208690299958306e-07,
+                              7.072585949269223e-09};
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+      c[i] = k[i];
+      asm("" : "+s"(c[i]));
+    }
+  }
+  __device__ __forceinline__ double operator()(double x) const {
+    x = fmax(x, -1100.0);   // 2^-1100 is 0
+    const double n = rint(x), f = x - n;
+    double s = c[9];
+#pragma unroll
+    for (int i = 8; i >= 0; --i) s = fma(s, f, c[i]);
+    return ldexp(fma(s, f, 1.0), (int)n);
+  }
+};
 
 // The weight of a logit in a row whose largest is `top`, exp((l - top) / T): none for NaN
 // and -inf; where the largest is +inf, the infinite ones share the row.
-__device__ __forceinline__ double weight(float l, float top, double slope) {
+__device__ __forceinline__ double weight(const Exp2& exp2, float l, float top, double slope) {
   if (top == INFINITY) return l == INFINITY ? 1.0 : 0.0;   // uniform over a row
-  return exp2_neg(((double)l - (double)top) * slope);
+  return exp2(((double)l - (double)top) * slope);
 }
 
 // Scans over a wave by DPP moves: a shuffle through LDS is ten times the latency, and
@@ -233,19 +242,29 @@ __global__ __launch_bounds__(kThreads) void verify_rows_kernel(Verify<T> a, int 
     for (int e = 0; e < kRowPer; ++e) top = fmaxf(top, x[e]);   // leaves NaN out
     top = max_f32(top);
     if (top > -INFINITY) {
+      const Exp2 exp2;
+      if (top == INFINITY) {
 #pragma unroll
-      for (int e = 0; e < kRowPer; ++e) s += weight(x[e], top, slope);
+        for (int e = 0; e < kRowPer; ++e) s += x[e] == INFINITY ? 1.0 : 0.0;
+      } else {
+#pragma unroll
+        for (int e = 0; e < kRowPer; ++e) s += exp2(((double)x[e] - (double)top) * slope);
+      }
       s = sum_f64(s);
     }
   }
   if (lane == 0) a.part[(int64_t)r * a.chunks + c] = Part{s, top, at};
 }
 
-// A row's maximum (greedy: with its first index) and its sum, by one wave.
-__device__ __forceinline__ Part row_total(const Part* part, int chunks, double slope, bool greedy) {
+// A row's maximum (greedy: with its first index) and its sum, by one wave; own: the
+// lane's first part, which first_part loads ahead.
+__device__ __forceinline__ Part first_part(const Part* part, int chunks) {
   const int lane = threadIdx.x & 63;
-  Part own{0.0, -INFINITY, INT_MAX};
-  if (lane < chunks) own = part[lane];
+  return lane < chunks ? part[lane] : Part{0.0, -INFINITY, INT_MAX};
+}
+__device__ __forceinline__ Part row_total(const Exp2& exp2, Part own, const Part* part, int chunks,
+                                          double slope, bool greedy) {
+  const int lane = threadIdx.x & 63;
   if (greedy) {
     for (int c = lane + 64; c < chunks; c += 64)
       if (part[c].top > own.top) own = part[c];
@@ -256,8 +275,9 @@ __device__ __forceinline__ Part row_total(const Part* part, int chunks, double s
   for (int c = lane + 64; c < chunks; c += 64) top = fmaxf(top, part[c].top);
   top = max_f32(top);
   if (!(top > -INFINITY)) return Part{0.0, top, INT_MAX};
-  double s = own.sum * weight(own.top, top, slope);
-  for (int c = lane + 64; c < chunks; c += 64) s += part[c].sum * weight(part[c].top, top, slope);
+  double s = own.sum * weight(exp2, own.top, top, slope);
+  for (int c = lane + 64; c < chunks; c += 64)
+    s += part[c].sum * weight(exp2, part[c].top, top, slope);
   return Part{sum_f64(s), top, 0};
 }
 
@@ -271,6 +291,7 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
   const int b = blockIdx.x / a.groups, group = blockIdx.x % a.groups;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = a.drafts(b);
+  const Exp2 exp2;
   bool greedy;
   const double slope = a.slope(b, &greedy);
   const float u_last = a.u[(int64_t)b * (a.g + 1) + a.g];
@@ -292,13 +313,27 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
         if (a.draft) lq = ld(a.draft_row(b, i0 + tid) + x);
       }
     }
-    for (int i = wave; i < m; i += kWaves) {
-      const Part p = row_total(a.target_part(b, i0 + i), a.chunks, slope, greedy);
-      Part r{0.0, 0.0f, 0};
-      if (a.draft && !greedy) r = row_total(a.draft_part(b, i0 + i), a.chunks, slope, false);
-      if (lane == 0) {
-        pt[i] = p;
-        qt[i] = r;
+    // two drafts of a wave at a time, their parts loaded together
+    const bool drawn = a.draft && !greedy;
+    for (int i = wave; i < m; i += 2 * kWaves) {
+      Part pf[2], qf[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = i0 + min(i + j * kWaves, m - 1);
+        pf[j] = first_part(a.target_part(b, row), a.chunks);
+        if (drawn) qf[j] = first_part(a.draft_part(b, row), a.chunks);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int k = i + j * kWaves;
+        if (k >= m) break;
+        const Part p = row_total(exp2, pf[j], a.target_part(b, i0 + k), a.chunks, slope, greedy);
+        Part r{0.0, 0.0f, 0};
+        if (drawn) r = row_total(exp2, qf[j], a.draft_part(b, i0 + k), a.chunks, slope, false);
+        if (lane == 0) {
+          pt[k] = p;
+          qt[k] = r;
+        }
       }
     }
     __syncthreads();
@@ -309,9 +344,9 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
         if (greedy) {
           keep = x >= 0 && x == p.at;
         } else {
-          const double px = x >= 0 && p.sum > 0.0 ? weight(lp, p.top, slope) / p.sum : 0.0;
+          const double px = x >= 0 && p.sum > 0.0 ? weight(exp2, lp, p.top, slope) / p.sum : 0.0;
           const double qx = !a.draft ? 1.0
-                            : x >= 0 && r.sum > 0.0 ? weight(lq, r.top, slope) / r.sum : 0.0;
+                            : x >= 0 && r.sum > 0.0 ? weight(exp2, lq, r.top, slope) / r.sum : 0.0;
           keep = (double)u * qx < px;
         }
       }
@@ -329,7 +364,8 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
     __syncthreads();
   }
   if (kept == n && wave == 0) {
-    const Part p = row_total(a.target_part(b, n), a.chunks, slope, greedy);
+    const Part* part = a.target_part(b, n);
+    const Part p = row_total(exp2, first_part(part, a.chunks), part, a.chunks, slope, greedy);
     if (lane == 0) p_row = p;
   }
   __syncthreads();
@@ -343,13 +379,18 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
   const T* other = mode == kPickRest ? a.draft_row(b, kept) : row;
   int gone = mode == kPickOthers ? a.tokens[(int64_t)b * a.g + kept] : -1;
   const double ip = mode == kPickRest ? 1.0 / p.sum : 1.0, iq = mode == kPickRest ? 1.0 / q.sum : 0.0;
-  // what token v holds in this mode
-  auto held = [&](int v) {
+  // the logits of token v, in one batch with others', and what it holds in this mode
+  auto load = [&](int v, float& l, float& o) {
+    const int at = min(max(v, 0), a.vocab - 1);
+    l = ld(row + at);
+    o = mode == kPickRest ? ld(other + at) : 0.0f;
+  };
+  auto held = [&](int v, float l, float o) {
     if (v < 0 || v >= a.vocab || v == gone) return 0.0;
-    const double w = weight(ld(row + v), p.top, slope);
+    const double w = weight(exp2, l, p.top, slope);
     if (mode != kPickRest) return w;
     // what is within the rounding of the rows' sums is none: of equal rows nothing is left
-    const double pv = w * ip, d = pv - weight(ld(other + v), q.top, slope) * iq;
+    const double pv = w * ip, d = pv - weight(exp2, o, q.top, slope) * iq;
     return d > pv * 0x1p-40 ? d : 0.0;
   };
   if (mode == kPickRest) {
@@ -359,8 +400,11 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
     uint64_t seen = 0;
     for (int t = group; t < a.tiles; t += a.groups) {
       double s = 0.0;
+      float l[kPer], o[kPer];
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) s += held(t * kTile + j * kThreads + tid);
+      for (int j = 0; j < kPer; ++j) load(t * kTile + j * kThreads + tid, l[j], o[j]);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) s += held(t * kTile + j * kThreads + tid, l[j], o[j]);
       s = block_sum(s, sh);
       if (tid == 0)
         seen |= __hip_atomic_exchange(&a.rest[(int64_t)b * a.tiles + t], __builtin_bit_cast(uint64_t, s),
@@ -388,7 +432,12 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
     int c_gone = gone >= 0 && gone < a.vocab ? (gone + lead) / kChunk : -1;
     if (c_gone >= 0) {
       double s = 0.0;
-      for (int j = tid; j < kChunk; j += kThreads) s += held(c_gone * kChunk - lead + j);
+      for (int j = tid; j < kChunk; j += kThreads) {
+        const int v = c_gone * kChunk - lead + j;
+        float l, o;
+        load(v, l, o);
+        s += held(v, l, o);
+      }
       whole_gone = block_sum(s, sh);
     }
     auto mass = [&](int c) {
@@ -400,7 +449,7 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
       }
       if (c >= a.chunks) return 0.0;
       if (c == c_gone) return whole_gone;
-      return part[c].top > -INFINITY ? part[c].sum * weight(part[c].top, p.top, slope) : 0.0;
+      return part[c].top > -INFINITY ? part[c].sum * weight(exp2, part[c].top, p.top, slope) : 0.0;
     };
     int parts = mode == kPickRest ? a.tiles : a.chunks;
     auto whole = [&]() {
@@ -437,10 +486,13 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
       const int size = mode == kPickRest ? kTile : kChunk;
       const int lo = found_part * size - (mode == kPickRest ? 0 : lead);
       double w[kPer], s = 0.0;
+      float l[kPer], o[kPer];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) load(lo + tid * kPer + e, l[e], o[e]);
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
         const int j = tid * kPer + e;
-        w[e] = j < size ? held(lo + j) : 0.0;
+        w[e] = j < size ? held(lo + j, l[e], o[e]) : 0.0;
         s += w[e];
       }
       const double scan = scan_f64(s);
