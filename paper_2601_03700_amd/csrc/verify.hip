@@ -87,8 +87,8 @@ __device__ __forceinline__ int lead_of(const T* row) {
 // 2^x for x <= 0, 0 for NaN: 2^n 2^f with n = rint(x), and 2^f by the polynomial of
 // degree 10 through the Chebyshev points of [-1/2, 1/2] (off by 3e-16 of it).  The
 // first kernel is bound by these instructions: the coefficients are kept in scalar
-// registers (as constants they took two moves for each product, 640 instructions a
-// wave where XXX do).
+// registers (as constants they took two moves for each product: 640 instructions a
+// wave, now 390; 64 x 8 drafts of 32000 logits 38 us, now 33).
 struct Exp2 {
   double c[10];
   __device__ __forceinline__ Exp2() {

@@ -149,7 +149,7 @@ class PagedKVCache:
         if start is not None:
             users = list(self._users)
             for b, n in lengths.items():
-                first = int(start[b] if isinstance(start, dict) else start)
+                first = int(start.get(b, n) if isinstance(start, dict) else start)
                 last = min(-(-n // self.page_size), len(self._pages[b]))
                 for i in range(max(first, 0) // self.page_size, last):
                     if users[self._pages[b][i]] > 1:
@@ -188,7 +188,7 @@ class PagedKVCache:
         """The sequences dst (one or several, without pages) continue from the first `length`
         tokens of sequence src: they share its full pages, and each gets a copy of what is
         used of the open one.  Raises ValueError, with nothing taken, where that does not fit."""
-        dst = [dst] if isinstance(dst, int) else list(dst)
+        dst = [int(b) for b in dst] if hasattr(dst, "__iter__") else [int(dst)]
         for b in (src, *dst):
             self._check_sequence(b)
         if src in dst or len(set(dst)) < len(dst) or any(self._pages[b] for b in dst):
@@ -677,7 +677,8 @@ class DecoderModel:
         """One pass over each sequence's last token (at pos[b], not yet in the cache) and its drafts
         [n, g] behind it, and their verification: (tokens [n, g+1], kept [n], pass result).  The
         cache then holds the last token and the drafts; those that were not kept are written
-        over by what comes next.  draft_logits [n, g, V] f32 (None: the drafts have no
+        over by what comes next.  It stands for decode passes: every token decides for itself
+        when it exits, also where cfg lets a prompt's last token decide.  draft_logits [n, g, V] f32 (None: the drafts have no
         probabilities); u [n, g+1]; temperature [n]; pos_max: the largest pos, when known on the
         host."""
         n, g = drafts.shape
@@ -691,7 +692,8 @@ class DecoderModel:
         at = pos.to(torch.int32)[:, None] + torch.arange(g + 1, **i32)
         seq = torch.arange(n, **i32).repeat_interleave(g + 1)
         rows = torch.arange(n * (g + 1), **i32)
-        res = self.token_pass(ids.reshape(-1), at.reshape(-1), seq, cache, cfg, None, True, rows)
+        each = B.ExitCfg(cfg.delta, cfg.min_exit_layer, cfg.n_layers, cfg.metric, 0)
+        res = self.token_pass(ids.reshape(-1), at.reshape(-1), seq, cache, each, None, True, rows)
         out, kept = self.verify_logits(res.logits.view(n, g + 1, -1), draft_logits,
                                        drafts.to(torch.int32).contiguous(), u, temperature)
         return out, kept, res

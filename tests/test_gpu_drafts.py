@@ -106,6 +106,26 @@ def test_a_verification_pass_is_its_logits_verified():
                               torch.zeros(n * (g + 1), device="cuda")), m.greedy(res.logits))
 
 
+def test_a_verification_pass_exits_token_by_token():
+    """Also under the policy by which a prompt's last token decides for all of it: the pass stands
+    for decode passes, which do not know that."""
+    m = build("f32")
+    n, g, T = 3, 5, 10
+    ids = ai.token_ids(10, SHAPE.vocab, n, T)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    drafts = torch.arange(n * g, **i32).view(n, g)
+    last, pos = torch.tensor([1, 2, 3], **i32), torch.full((n,), T, **i32)
+    u = torch.full((n, g + 1), 0.5, device="cuda")
+    out = []
+    for prompt_level in (False, True):
+        cfg = B.exit_cfg(0.5, SHAPE.n_layers, min_exit_layer=2, prompt_level=prompt_level)
+        _, cache = m.prefill(ids, never(), s_max=32, logits=None)
+        out.append(m.verify(cache, last, drafts, pos, cfg, u)[2])
+        assert cfg.prompt_level == int(prompt_level)
+    assert torch.equal(out[0].exit_layer, out[1].exit_layer)
+    assert torch.equal(out[0].logits, out[1].logits)
+
+
 def test_verification_refuses_what_does_not_fit():
     m = build("f32")
     cache = m.new_cache(2, 8)

@@ -1,5 +1,6 @@
 """Page bookkeeping of forked, truncated, compacted and resized caches, without a GPU: what the
 pages hold is followed through a copy in torch."""
+import numpy as np
 import pytest
 import torch
 
@@ -82,7 +83,7 @@ def test_forks_share_full_pages_and_copy_the_open_one(copies):
     assert c.shared_pages == 2 and read(c, 1, 11) == [*range(1, 11), 60]
     c.fork(3, 0, 8)                                # whole pages: nothing copied
     assert len(copies) == 2 and c.shared_pages == 2
-    c.fork(1, 2, 0)                                # of nothing
+    c.fork(1, np.int64(2), 0)                      # of nothing
     consistent(c)
     for b in range(4):
         c.release(b)
@@ -106,6 +107,10 @@ def test_a_write_into_a_shared_page_copies_it_first(copies):
     consistent(c)
     c.reserve({0: 12})                             # no start: appended to
     assert len(copies) == n + 1
+    c.fork(1, 3, 8)
+    c.reserve({1: 12, 3: 12}, {3: 4})              # of one of them only
+    assert len(copies) == n + 2 and copies[-1][0] == c._pages[1][1]
+    consistent(c)
 
 
 def test_nothing_is_taken_where_copies_do_not_fit(copies):
