@@ -152,6 +152,10 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   auto hi_of = [&](int s) { return min((w0 + s + 1) * sp.U - u0, KT); };
   const char* br[NB];
   [[maybe_unused]] const uint8_t* sr[NB];
+  // Q4: a lane's place in a block of codes; the block is the wave's but where two kinds
+  // share it, so that the loads have a scalar address
+  constexpr bool kShared = NB == 1 && (EPI == EPI_SWIGLU || EPI == EPI_QKV);
+  [[maybe_unused]] const uint32_t code_at = (uint32_t)(r16 * 16 + q * 256), scale_at = r16 * 4;
 #pragma unroll
   for (int x = 0; x < NB; ++x) {
     const bool second = pair && (NB == 1 ? r16 >= 8 : x >= HALF);   // a lane of the second kind
@@ -160,9 +164,16 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
     const bool b2 = EPI == EPI_SWIGLU && second;
     if constexpr (Q4) {
       // a block of columns behind the last (plain stores): the last one's, not stored
-      const int64_t blk = (int64_t)min(row >> 4, (p.N - 1) >> 4) * KT;
-      br[x] = (const char*)(b2 ? qv.codes2 : qv.codes) + blk * kQuantBlock + (row & 15) * 16 + q * 256;
-      sr[x] = (b2 ? qv.scales2 : qv.scales) + blk * kQuantScales + (row & 15) * 4;
+      int at = row >> 4;
+      if constexpr (!kShared)
+        at = (n0 >> 4) + (NB > 1 && pair ? x % HALF + (second && EPI != EPI_SWIGLU ? dn >> 4 : 0) : x);
+      const int64_t blk = (int64_t)min(at, (p.N - 1) >> 4) * KT;
+      br[x] = (const char*)(b2 ? qv.codes2 : qv.codes) + blk * kQuantBlock;
+      sr[x] = (b2 ? qv.scales2 : qv.scales) + blk * kQuantScales;
+      if constexpr (kShared) {   // the row of the block that the lane has is not r16
+        br[x] += ((row & 15) - r16) * 16;
+        sr[x] += ((row & 15) - r16) * 4;
+      }
     } else {
       br[x] = (const char*)((b2 ? p.B2 : p.B) + (int64_t)row * p.ldb + 8 * q);
     }
@@ -180,9 +191,9 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
 #pragma unroll
       for (int x = 0; x < NB; ++x) {
         if constexpr (Q4) {
-          const u32x4_t* w = reinterpret_cast<const u32x4_t*>(br[x] + (int64_t)c * kQuantBlock);
+          const u32x4_t* w = reinterpret_cast<const u32x4_t*>(br[x] + (int64_t)c * kQuantBlock + code_at);
           bw[st][u][x][0] = again ? *w : __builtin_nontemporal_load(w);
-          sw[st][u][x] = *reinterpret_cast<const uint32_t*>(sr[x] + (int64_t)c * kQuantScales);
+          sw[st][u][x] = *reinterpret_cast<const uint32_t*>(sr[x] + (int64_t)c * kQuantScales + scale_at);
         } else {
 #pragma unroll
           for (int h = 0; h < HS; ++h)
@@ -266,12 +277,12 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int j = i / kLoads;
-      const int64_t at = (int64_t)round * kSeg + i % kLoads * 1024 + lane * 16;
+      const int at = round * kSeg + i % kLoads * 1024;
       // rows that are not there and K behind the last are zeros: the codes there are
       // too, but 0 times what memory holds might be NaN
       xw[i] = u32x4_t{0, 0, 0, 0};
-      if (m0 + kRowsW * wave + j < M && at < 2 * (int64_t)p.K)
-        xw[i] = *reinterpret_cast<const u32x4_t*>(xr[j] + at);
+      if (m0 + kRowsW * wave + j < M && lane * 16 < 2 * p.K - at)
+        xw[i] = *reinterpret_cast<const u32x4_t*>(xr[j] + at + (uint32_t)(lane * 16));
     }
   };
   [[maybe_unused]] auto store_x = [&](int buf) {
