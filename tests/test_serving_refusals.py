@@ -128,3 +128,69 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         B._logit_rows("x", torch.zeros(2, 4, 12)[:, :3, :10], 2, 3, 10)
     assert B._logit_rows("x", torch.zeros(2, 3, 12)[:, :, :10], 2, 3, 10) == 12
     assert B._logit_rows("x", torch.zeros(2, 4, 10)[:, :1], 2, 1, 10) == 40
+
+
+def layer_args(**change):
+    a = B.LayerArgs()
+    for name, kind in B.LayerArgs._fields_:
+        if kind is ctypes.c_void_p:
+            setattr(a, name, A)
+    a.dtype, a.n_layers, a.d_model, a.n_heads, a.head_dim, a.d_ff = B.BF16, 4, 256, 4, 64, 512
+    a.family, a.rms_eps, a.exit = 0, 1e-6, B.exit_cfg(0.9, 4)
+    a.n_tok = a.max_active = a.n_seq = a.n_slots = 8
+    a.s_max = a.rope_max_pos = 1
+    a.hsm = None
+    a.active[0], a.active[1], a.n_active[0], a.n_active[1] = A, 2 * A, A, 2 * A
+    a.h[0], a.h[1] = A, 2 * A
+    a.workspace_bytes = 1 << 40
+    for k, v in change.items():
+        setattr(a, k, v)
+    return a
+
+
+def layer_weights(**change):
+    w = B.QuantLayers()
+    for name, _ in B.QuantLayers._fields_:
+        setattr(w, name, change.get(name, B.QuantMat(A, A)))
+    return w
+
+
+def step(a, w, kv_=None, table=None, pages=0, layer=1):
+    ref = lambda x: None if x is None else ctypes.byref(x)
+    return B.lib().adept_layer_step_quant(ref(a), ref(w), ref(kv_), table, pages, None, layer, None)
+
+
+def test_layer_steps_refuse():
+    assert step(None, layer_weights()) == -1 and step(layer_args(), None) == -1
+    assert step(layer_args(dtype=B.F32), layer_weights()) == -1
+    for name in ("qkv", "o", "gate", "up", "down"):
+        for bad in (B.QuantMat(None, A), B.QuantMat(A, None), B.QuantMat(A + 8, A), B.QuantMat(A, A + 4)):
+            assert step(layer_args(), layer_weights(**{name: bad})) == -1, name
+            assert b"codes and scales" in B.lib().adept_last_error()
+    assert step(layer_args(), layer_weights(), layer=5) == -1
+    # the GPT2 family has no second projection of that kind
+    assert step(layer_args(family=B.FAMILY_GPT2, d_ff=100), layer_weights(up=B.QuantMat())) == -1
+    assert b"codes and scales" not in B.lib().adept_last_error()
+    # over pages: the checks of the paged step
+    assert step(layer_args(), layer_weights(), kv(n_kv_heads=2)) == -1
+    assert b"heads" in B.lib().adept_last_error()
+    assert step(layer_args(), layer_weights(), kv(n_kv_heads=4), None, 4) == -1
+    assert b"page table" in B.lib().adept_last_error()
+    need = B.lib().adept_layer_quant_workspace_bytes(ctypes.byref(layer_args()),
+                                                     ctypes.byref(layer_weights()), None, 0)
+    assert need > 0
+    assert step(layer_args(workspace_bytes=need - 1), layer_weights()) == -3
+    assert B.lib().adept_layer_quant_workspace_bytes(None, None, None, 0) == 0
+
+
+def test_heads_refuse():
+    f = B.lib().adept_final_logits_quant
+    good = [256, 100, 1e-6, A, A, A, A, A, 4, A, None, A, A, A, A, None]
+    for i, bad in ((0, 252), (0, 0), (1, 0), (3, None), (4, None), (5, None), (6, None), (8, -1),
+                   (9, None), (11, None), (12, A + 8), (13, None), (14, A + 8), (10, A + 2), (3, A + 8)):
+        args = list(good)
+        args[i] = bad
+        assert f(*args) == -1, (i, bad)
+    args = list(good)
+    args[8] = 0
+    assert f(*args) == 0
