@@ -31,6 +31,9 @@ namespace adept {
 namespace {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+// in global memory: a pointer put together from two words is a flat one otherwise, whose
+// loads go through the LDS counter too
+typedef __attribute__((address_space(1))) u32x4_t global_u32x4_t;
 
 // What the epilogue of one thread's four columns (n.. of row m) reads, loaded
 // beside the first operands: each would be one more memory latency at the end.
@@ -282,7 +285,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
       // too, but 0 times what memory holds might be NaN
       xw[i] = u32x4_t{0, 0, 0, 0};
       if (m0 + kRowsW * wave + j < M && lane * 16 < 2 * p.K - at)
-        xw[i] = *reinterpret_cast<const u32x4_t*>(xr[j] + at + (uint32_t)(lane * 16));
+        xw[i] = *reinterpret_cast<const global_u32x4_t*>((uintptr_t)xr[j] + at + (uint32_t)(lane * 16));
     }
   };
   [[maybe_unused]] auto store_x = [&](int buf) {

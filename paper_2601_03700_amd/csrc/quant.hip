@@ -134,7 +134,7 @@ __global__ __launch_bounds__(64 * kWaves) void quant_unpack_kernel(
 }
 
 adept_status check_matrix(const char* what, int n, int k, const void* codes, const void* scales) {
-  ADEPT_REQUIRE(n > 0 && k > 0 && n <= INT_MAX - kQuantRows && k <= INT_MAX - kQuantK,
+  ADEPT_REQUIRE(n > 0 && k > 0 && n <= INT_MAX - kQuantRows && k <= 1 << 29,
                 "%s: bad sizes", what);
   ADEPT_REQUIRE(quant_blocks(n, k) <= (int64_t)kWaves << 23, "%s: a matrix of %d x %d is too large",
                 what, n, k);   // a grid's bound

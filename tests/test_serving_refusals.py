@@ -49,7 +49,8 @@ def unpack(dt=B.BF16, n=20, k=40, w=A, ldw=40, codes=A, scales=A):
 @pytest.mark.parametrize("call", [pack, unpack])
 @pytest.mark.parametrize("bad", [dict(dt=2), dict(n=0), dict(k=0), dict(n=2**31 - 1), dict(w=None),
                                  dict(ldw=39), dict(codes=None), dict(scales=None), dict(codes=A + 8),
-                                 dict(scales=A + 4), dict(w=A + 1), dict(n=1 << 30, k=1 << 10, ldw=1 << 10)],
+                                 dict(scales=A + 4), dict(w=A + 1), dict(n=1 << 30, k=1 << 10, ldw=1 << 10),
+                                 dict(k=(1 << 29) + 8, ldw=1 << 30)],
                          ids=str)
 def test_pack_refuses(call, bad):
     assert call(**bad) == -1
