@@ -175,13 +175,23 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
   return s;
 }
 
+// Loads from global memory: a row chosen among two is a flat pointer otherwise, whose
+// loads wait for each other.
+__device__ __forceinline__ float load_one(const float* p) {
+  return *(const __attribute__((address_space(1))) float*)(uintptr_t)p;
+}
+__device__ __forceinline__ float load_one(const bf16* p) {
+  return bf2f(*(const __attribute__((address_space(1))) bf16*)(uintptr_t)p);
+}
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(1))) u32x4_t global_u32x4_t;
 __device__ __forceinline__ void load_vec(const float* p, float* x) {
-  const float4 w = *reinterpret_cast<const float4*>(p);
-  x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+  const u32x4_t w = *(const global_u32x4_t*)(uintptr_t)p;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
 }
 __device__ __forceinline__ void load_vec(const bf16* p, float* x) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  const u32x4_t u = *(const global_u32x4_t*)(uintptr_t)p;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[2 * e] = __uint_as_float(u[e] << 16);
@@ -225,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void verify_rows_kernel(Verify<T> a, int 
     } else {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        x[j * VEC + e] = v + e >= 0 && v + e < a.vocab ? ld(row + v + e) : -INFINITY;
+        x[j * VEC + e] = v + e >= 0 && v + e < a.vocab ? load_one(row + v + e) : -INFINITY;
     }
   }
   float top = -INFINITY;
@@ -385,8 +395,8 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(Verify<T> a) {
   // the logits of token v, in one batch with others', and what it holds in this mode
   auto load = [&](int v, float& l, float& o) {
     const int at = min(max(v, 0), a.vocab - 1);
-    l = ld(row + at);
-    o = mode == kPickRest ? ld(other + at) : 0.0f;
+    l = load_one(row + at);
+    o = mode == kPickRest ? load_one(other + at) : 0.0f;
   };
   auto held = [&](int v, float l, float o) {
     if (v < 0 || v >= a.vocab || v == gone) return 0.0;
