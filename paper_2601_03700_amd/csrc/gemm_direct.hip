@@ -271,7 +271,7 @@ __global__ __launch_bounds__(64 * W) void gemm_direct_kernel(GP p, RowList rl, i
   };
   // Q4: the activations of a round of pieces (one for each wave) go through LDS, where a
   // wave brings 16 / W rows of them in 1 KiB loads: straight from global memory to the
-  // operands, 64 bytes of 16 rows a load, 16 rows of 4096 x 11008 took 14.2 us, 9.8 so.
+  // operands, 64 bytes of 16 rows a load, 16 rows of 4096 x 11008 took 14.2 us, 9.3 so.
   constexpr int kSeg = W * 256, kXRow = kSeg + 16;      // bytes of a row in a round, in LDS
   constexpr int kRowsW = 16 / W < 1 ? 1 : 16 / W, kLoads = 4 / kRowsW < 1 ? 1 : 4 / kRowsW;
   [[maybe_unused]] u32x4_t xw[4];
