@@ -492,8 +492,9 @@ adept_status adept_verify_drafts(adept_dtype dt, int n_seq, int max_draft, int v
  * *n_rows (<= max_rows; NULL: exactly max_rows), later rows of y left as they were.
  * x [.][k] bf16, rows x_stride elements apart, 16-byte aligned; k and x_stride
  * multiples of 8; bias [n] bf16, nullable; y [max_rows][n] out_dt, rows y_stride
- * apart, any alignment.  Products of bf16 numbers, sums in f32.  The weights are
- * read once for every 64 rows: for many rows the unpacked matrix is faster.
+ * apart, any alignment.  Products of bf16 numbers, sums in f32.  The weights are read
+ * (past the first time from cache) and converted for every 16 rows: for many rows
+ * the unpacked matrix is faster.
  * ------------------------------------------------------------------------- */
 size_t adept_quant_codes_bytes(int n, int k);
 size_t adept_quant_scales_bytes(int n, int k);
