@@ -230,21 +230,25 @@ class PagedKVCache:
 
     def resize(self, n_pages):
         """Another number of pages: more of them, or memory given back after a peak (pages in use
-        behind the new end are moved first).  Descriptors of the old tensors are no longer the
-        cache's.  Raises ValueError where more pages are in use."""
+        behind the new end are moved first).  The old tensors and the new ones are held together
+        for the time of the call, and descriptors of the old ones are no longer the cache's.
+        Raises ValueError where more pages are in use; what fails for want of memory leaves the
+        cache as it was."""
         used = self.n_pages - len(self._free)
         if n_pages < used or n_pages < 1:
             raise ValueError(f"{n_pages} pages, {used} in use")
+        held = {name: getattr(self, name) for name in ("k", "v", "k_scale", "v_scale")}
+        new = {name: old if old is None else
+               torch.empty((old.shape[0], (n_pages + 1) * self.page_size, *old.shape[2:]),
+                           dtype=old.dtype, device=old.device) for name, old in held.items()}
         if n_pages < self.n_pages:
             self._move(n_pages)
         keep = min(n_pages, self.n_pages) * self.page_size
-        for name in ("k", "v", "k_scale", "v_scale"):
-            old = getattr(self, name)
+        for name, old in held.items():
             if old is not None:
-                new = torch.empty((old.shape[0], (n_pages + 1) * self.page_size, *old.shape[2:]),
-                                  dtype=old.dtype, device=old.device)
-                new[:, :keep] = old[:, :keep]
-                setattr(self, name, new)
+                new[name][:, :keep] = old[:, :keep]
+        for name, t in new.items():
+            setattr(self, name, t)
         self._users = (self._users + [0] * (n_pages - self.n_pages))[:n_pages]
         self._free = [p for p in range(n_pages - 1, -1, -1) if not self._users[p]]
         self.kv = self.layer_kv(1)
