@@ -131,6 +131,16 @@ class PagedKVCache:
             B.paged_copy(self.kv, self.k.shape[0], up(src), up(dst),
                          None if n_tokens is None else up(n_tokens))
 
+    def _take_copies(self, src, n_tokens=None):
+        """New pages with what the pages src hold; none are taken where the copy fails."""
+        new = self._take(len(src))
+        try:
+            self._copy(src, new, n_tokens)
+        except BaseException:
+            self._give(new)
+            raise
+        return new
+
     def reserve(self, lengths, start=None):
         """Pages for lengths[b] tokens of sequence b (a dict or one number for all); start[b]: the
         position from which on they are going to be written (a dict or one number; None: behind
@@ -157,8 +167,7 @@ class PagedKVCache:
                         own.append((b, i))
         if need + len(own) > len(self._free):
             raise ValueError(f"{need + len(own)} more pages needed, {len(self._free)} free")
-        new = self._take(len(own))
-        self._copy([self._pages[b][i] for b, i in own], new)
+        new = self._take_copies([self._pages[b][i] for b, i in own])
         for (b, i), page in zip(own, new):
             self._give([self._pages[b][i]])
             self._pages[b][i] = page
@@ -199,9 +208,8 @@ class PagedKVCache:
                              f"{len(self._pages[src]) * self.page_size}")
         if left and len(dst) > len(self._free):
             raise ValueError(f"{len(dst)} more pages needed, {len(self._free)} free")
-        new = self._take(len(dst)) if left else []
-        if new:
-            self._copy([self._pages[src][full]] * len(new), new, [left] * len(new))
+        new = (self._take_copies([self._pages[src][full]] * len(dst), [left] * len(dst)) if left
+               else [])
         for k, b in enumerate(dst):
             self._pages[b] = self._pages[src][:full] + new[k:k + 1]
             for p in self._pages[b][:full]:

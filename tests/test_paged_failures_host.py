@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2601_03700_amd import binding as B
 from paper_2601_03700_amd import model as M
 from tests.test_paged_share_host import PAGE, cache, consistent, copies, own, read, write  # noqa: F401
 
@@ -46,3 +47,54 @@ def test_a_resize_without_memory_changes_nothing(monkeypatch, kv, at, n_pages):
     for t in (c.k, c.v, c.k_scale, c.v_scale):
         assert t is None or t.shape[1] == (n_pages + 1) * PAGE
     assert all(read(c, b, 9) == w for b, w in want.items())
+
+
+@pytest.fixture
+def no_copies(monkeypatch, copies):                        # noqa: F811
+    def fail(*args, **kw):
+        raise B.AdeptError("no copy")
+
+    return lambda m: m.setattr(B, "paged_copy", fail)
+
+
+def state(c):
+    return ([list(p) for p in c._pages], list(c._users), list(c._free), c.shared_pages,
+            c.page_table.tolist())
+
+
+def test_a_copy_that_fails_takes_no_pages(monkeypatch, no_copies):
+    c = own(cache())
+    write(c, 0, 0, range(1, 11))
+    c.fork(0, 2, 8)                                # two shared pages, seven free
+    calls = [lambda: c.fork(0, [1, 3], 10),        # the open page for each
+             lambda: c.reserve({2: 13}, 3),        # both shared pages, and two more
+             lambda: c.reserve({0: 10, 2: 8}, 4)]  # of the first of the two
+    for call in calls:
+        then = state(c)
+        with monkeypatch.context() as m:
+            no_copies(m)
+            with pytest.raises(B.AdeptError, match="no copy"):
+                call()
+        assert state(c) == then
+        consistent(c)
+    for call in calls:                             # and all of it is there for the next ones
+        call()
+        consistent(c)
+    assert read(c, 0, 10) == read(c, 1, 10) == read(c, 3, 10) == list(range(1, 11))
+    assert read(c, 2, 8) == list(range(1, 9))
+
+
+def test_a_move_that_fails_moves_nothing(monkeypatch, no_copies):
+    c = own(cache(n_pages=12))
+    for b in range(4):
+        write(c, b, 0, [10 * b + i for i in range(9)])
+    c.release(0)
+    for call in (c.compact, lambda: c.resize(9)):
+        then = state(c), c.k, c.v, c.kv
+        with monkeypatch.context() as m:
+            no_copies(m)
+            with pytest.raises(B.AdeptError, match="no copy"):
+                call()
+        assert state(c) == then[0] and (c.k is then[1] and c.v is then[2] and c.kv is then[3])
+        assert all(read(c, b, 9) == [10 * b + i for i in range(9)] for b in (1, 2, 3))
+        consistent(c)
