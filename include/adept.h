@@ -464,6 +464,7 @@ adept_status adept_paged_copy(const adept_paged_kv* kv, int n_layers, const int3
  *  workspace: adept_verify_drafts_workspace_bytes(n_seq, max_draft, vocab) bytes,
  *  16-byte aligned; its contents on entry do not matter.  Calls that may overlap
  *  need their own.
+ *  A call has n_seq (2 max_draft + 1) ceil((vocab + 7) / 1024) < 2^24.
  * ------------------------------------------------------------------------- */
 size_t adept_verify_drafts_workspace_bytes(int n_seq, int max_draft, int vocab);
 adept_status adept_verify_drafts(adept_dtype dt, int n_seq, int max_draft, int vocab,
@@ -487,6 +488,7 @@ adept_status adept_verify_drafts(adept_dtype dt, int n_seq, int max_draft, int v
  * codes and scales, adept_quant_codes_bytes(n, k) / _scales_bytes(n, k) bytes in
  * this library's own order (blocks of 16 rows and 128 of k, filled up with zeros),
  * 16-byte aligned.  Matrices of one shape may be stacked.  adept_quant_unpack: back.
+ * k is at most 2^29, a matrix at most 2^25 blocks.
  *
  * adept_quant_linear: y[i] = x[row] w^T + bias, row = rows ? rows[i] : i, for i <
  * *n_rows (<= max_rows; NULL: exactly max_rows), later rows of y left as they were.
@@ -494,7 +496,8 @@ adept_status adept_verify_drafts(adept_dtype dt, int n_seq, int max_draft, int v
  * multiples of 8; bias [n] bf16, nullable; y [max_rows][n] out_dt, rows y_stride
  * apart, any alignment.  Products of bf16 numbers, sums in f32.  The weights are read
  * (past the first time from cache) and converted for every 16 rows: for many rows
- * the unpacked matrix is faster.
+ * the unpacked matrix is faster.  A call has
+ * (ceil(n / 16) + 7) ceil(max_rows / 16) < 2^22 and max_rows <= 64 * 65535.
  * ------------------------------------------------------------------------- */
 size_t adept_quant_codes_bytes(int n, int k);
 size_t adept_quant_scales_bytes(int n, int k);
@@ -508,7 +511,8 @@ adept_status adept_quant_linear(int n, int k, const void* x, int64_t x_stride, c
                                 int64_t y_stride, void* stream);
 
 /* adept_final_logits (norm_bias NULL) or adept_final_logits_layernorm (else) with
- * the head [vocab][d_model] in 4 bits; bf16 states, d_model a multiple of 8. */
+ * the head [vocab][d_model] in 4 bits; bf16 states, d_model a multiple of 8; vocab
+ * and max_rows within adept_quant_linear's bounds (n, max_rows). */
 adept_status adept_final_logits_quant(int d_model, int vocab, float eps, const void* h0_buf,
                                       const void* h1_buf, const int32_t* exit_layer,
                                       const int32_t* rows, const int32_t* n_rows, int max_rows,

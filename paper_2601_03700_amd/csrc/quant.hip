@@ -143,6 +143,14 @@ adept_status check_matrix(const char* what, int n, int k, const void* codes, con
   return ADEPT_OK;
 }
 
+// Rows of a product with n weight rows: a grid's bound, of workgroups of up to 1024 threads.
+adept_status check_rows(const char* what, int n, int max_rows) {
+  ADEPT_REQUIRE(max_rows >= 0 && max_rows <= 64 * 65535 &&
+                    (ceil_div(n, 16) + 7ll) * ceil_div(max_rows, 16) < 1 << 22,
+                "%s: bad max_rows %d", what, max_rows);
+  return ADEPT_OK;
+}
+
 }  // namespace
 }  // namespace adept
 
@@ -198,10 +206,7 @@ extern "C" adept_status adept_quant_linear(int n, int k, const void* x, int64_t 
   ADEPT_REQUIRE(out_dt == ADEPT_F32 || out_dt == ADEPT_BF16, "quant_linear: bad dtype");
   ADEPT_TRY(check_matrix("quant_linear", n, k, codes, scales));
   ADEPT_REQUIRE(k % 8 == 0, "quant_linear: k = %d is no multiple of 8", k);
-  // a grid's bound: workgroups of up to 1024 threads
-  ADEPT_REQUIRE(max_rows >= 0 && max_rows <= 64 * 65535 &&
-                    (ceil_div(n, 16) + 7ll) * ceil_div(max_rows, 16) < 1 << 22,
-                "quant_linear: bad max_rows %d", max_rows);
+  ADEPT_TRY(check_rows("quant_linear", n, max_rows));
   if (max_rows == 0) return ADEPT_OK;
   ADEPT_REQUIRE(x && y && aligned16(x) && x_stride >= k && x_stride % 8 == 0,
                 "quant_linear: x must be 16-byte aligned rows, a multiple of 16 bytes apart");
@@ -223,10 +228,11 @@ extern "C" adept_status adept_final_logits_quant(int d_model, int vocab, float e
                                                  const void* norm_gain, const void* norm_bias,
                                                  const void* codes, const void* scales, void* x_norm,
                                                  float* logits, void* stream) {
-  ADEPT_REQUIRE(max_rows >= 0 && d_model % 8 == 0, "final_logits_quant: bad sizes");
+  ADEPT_REQUIRE(d_model % 8 == 0, "final_logits_quant: bad sizes");
   ADEPT_REQUIRE(h0_buf && h1_buf && exit_layer && rows && norm_gain && x_norm && logits,
                 "final_logits_quant: NULL tensor");
   ADEPT_TRY(check_matrix("final_logits_quant", vocab, d_model, codes, scales));
+  ADEPT_TRY(check_rows("final_logits_quant", vocab, max_rows));
   ADEPT_REQUIRE(aligned16(h0_buf) && aligned16(h1_buf) && aligned16(x_norm) && aligned16(logits) &&
                     aligned16(norm_gain) && aligned16(norm_bias),
                 "final_logits_quant: tensors must be 16-byte aligned");
