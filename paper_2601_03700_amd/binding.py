@@ -671,6 +671,11 @@ def quant_unpack(qw, w, mat=0, stream=None):
                                     stream_handle(stream)), "adept_quant_unpack")
 
 
+def quant_linear_max_rows(n):
+    """The most rows that a call (quant_linear, final_logits_quant) takes over n weight rows."""
+    return min(64 * 65535, ((1 << 22) - 1) // (-(-n // 16) + 7) * 16)
+
+
 def quant_linear(x, qw, y, mat=0, rows=None, n_rows=None, bias=None, stream=None):
     """y[i] = x[row] w^T + bias with matrix `mat` of qw, row = rows[i] (None: i); n_rows (device
     int32 [1]): how many.  x bf16 [m, k], y f32 or bf16 [rows, n], any row stride."""

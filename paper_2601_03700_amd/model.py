@@ -588,25 +588,33 @@ class DecoderModel:
         if logit_rows is None:
             return PassResult(None, None, st.exit_layer, st)
         rows = logit_rows.to(torch.int32)
-        nr = int(rows.shape[0])
-        n_rows = torch.tensor([nr], dtype=torch.int32, device=self.device)
+        return PassResult(self._head(st, rows), rows, st.exit_layer, st)
+
+    def _head(self, st, rows):
+        """Logits of the listed rows of a pass, from their states at their exits."""
+        s, nr = self.shape, int(rows.shape[0])
+        count = lambda n: torch.tensor([n], dtype=torch.int32, device=self.device)
         logits = torch.empty((nr, s.vocab), dtype=torch.float32, device=self.device)
         xn = torch.empty((nr, s.d_model), dtype=self.tdt, device=self.device)
         # (the bf16 GEMMs take a vocabulary that is a multiple of 64)
         if self.quant is not None and (nr <= 64 or s.vocab % 64):
             gain, bias = ((self.final_ln_g, self.final_ln_b) if self.gpt2
                           else (self.final_norm, None))
-            B.final_logits_quant(s.d_model, s.vocab, s.ln_eps if self.gpt2 else s.rms_eps, st.h[0],
-                                 st.h[1], st.exit_layer, rows, n_rows, nr, gain, bias,
-                                 self.quant["lm_head"], xn, logits)
+            most = B.quant_linear_max_rows(s.vocab)
+            for i in range(0, nr, most):
+                m = min(most, nr - i)
+                B.final_logits_quant(s.d_model, s.vocab, s.ln_eps if self.gpt2 else s.rms_eps,
+                                     st.h[0], st.h[1], st.exit_layer, rows[i:i + m], count(m), m,
+                                     gain, bias, self.quant["lm_head"], xn[i:i + m],
+                                     logits[i:i + m])
         elif self.gpt2:
             B.final_logits_layernorm(s.d_model, s.vocab, s.ln_eps, st.h[0], st.h[1],
-                                     st.exit_layer, rows, n_rows, nr, self.final_ln_g,
+                                     st.exit_layer, rows, count(nr), nr, self.final_ln_g,
                                      self.final_ln_b, self.lm_head, xn, logits)
         else:
             B.final_logits(s.d_model, s.vocab, s.rms_eps, st.h[0], st.h[1], st.exit_layer, rows,
-                           n_rows, nr, self.final_norm, self.lm_head, xn, logits)
-        return PassResult(logits, rows, st.exit_layer, st)
+                           count(nr), nr, self.final_norm, self.lm_head, xn, logits)
+        return logits
 
     def prefill(self, ids, cfg, s_max=None, force_layer=None, logits="all", cache=None,
                 on_layer=None, start=0):
