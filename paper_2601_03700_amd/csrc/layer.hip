@@ -350,25 +350,28 @@ extern "C" adept_status adept_layer_step(const adept_layer_args* a, int layer, v
 
 namespace adept {
 namespace {
-adept_status check_paged_step(const adept_layer_args* a, const adept_paged_kv* kv,
-                              const int32_t* page_table, int max_pages, const int32_t* cache_slot) {
-  ADEPT_TRY(paged_check("layer_step_paged", (adept_dtype)a->dtype, kv));
+adept_status check_paged_step(const char* what, const adept_layer_args* a,
+                              const adept_paged_kv* kv, const int32_t* page_table, int max_pages,
+                              const int32_t* cache_slot) {
+  ADEPT_TRY(paged_check(what, (adept_dtype)a->dtype, kv));
   ADEPT_REQUIRE(kv->n_kv_heads == a->n_heads && kv->head_dim == a->head_dim,
-                "layer_step_paged: the cache's heads are not the layer's");
-  ADEPT_REQUIRE(a->n_layers >= 1 && a->n_tok <= kMaxEntries && a->n_seq > 0, "layer_step_paged: bad sizes");
+                "%s: the cache's heads are not the layer's", what);
+  ADEPT_REQUIRE(a->n_layers >= 1 && a->n_tok <= kMaxEntries && a->n_seq > 0,
+                "%s: bad sizes", what);
   ADEPT_REQUIRE(page_table && max_pages > 0 && (int64_t)max_pages * kv->page_size <= kMaxTokens,
-                "layer_step_paged: bad page table");
+                "%s: bad page table", what);
   if (kv->dtype == ADEPT_KV_FP8) {
-    ADEPT_REQUIRE(cache_slot != nullptr, "layer_step_paged: an FP8 cache needs the rows' slots");
-    ADEPT_REQUIRE(a->n_slots >= a->n_tok, "layer_step_paged: fewer K/V rows than rows of the pass");
+    ADEPT_REQUIRE(cache_slot != nullptr, "%s: an FP8 cache needs the rows' slots", what);
+    ADEPT_REQUIRE(a->n_slots >= a->n_tok,
+                  "%s: fewer K/V rows than rows of the pass", what);
     ADEPT_REQUIRE(aligned16(a->k_cache) && aligned16(a->v_cache),
-                  "layer_step_paged: the K/V rows must be 16-byte aligned");
+                  "%s: the K/V rows must be 16-byte aligned", what);
     // generated after layer N, the K/V of exited rows would miss their slots
     ADEPT_REQUIRE(a->attn_tiles || a->kv_fused,
-                  "layer_step_paged: a decode pass over an FP8 cache needs kv_fused");
+                  "%s: a decode pass over an FP8 cache needs kv_fused", what);
   } else {
     ADEPT_REQUIRE(a->k_cache == kv->k && a->v_cache == kv->v && a->n_slots == paged_slots(*kv),
-                  "layer_step_paged: the arguments' cache is not the paged one");
+                  "%s: the arguments' cache is not the paged one", what);
   }
   return ADEPT_OK;
 }
@@ -379,7 +382,7 @@ extern "C" adept_status adept_layer_step_paged(const adept_layer_args* a, const 
                                                const int32_t* page_table, int max_pages,
                                                const int32_t* cache_slot, int layer, void* stream) {
   ADEPT_REQUIRE(a != nullptr, "layer_step_paged: args is NULL");
-  ADEPT_TRY(check_paged_step(a, kv, page_table, max_pages, cache_slot));
+  ADEPT_TRY(check_paged_step("layer_step_paged", a, kv, page_table, max_pages, cache_slot));
   const PagedStep pg{kv, page_table, max_pages, cache_slot};
   return layer_step(a, layer, &pg, nullptr, stream);
 }
@@ -403,11 +406,11 @@ extern "C" adept_status adept_layer_step_quant(const adept_layer_args* a, const 
     ADEPT_REQUIRE(mats[i]->codes && mats[i]->scales && aligned16(mats[i]->codes) &&
                       aligned16(mats[i]->scales),
                   "layer_step_quant: codes and scales must be 16-byte aligned");
-  if (kv) ADEPT_TRY(check_paged_step(a, kv, page_table, max_pages, cache_slot));
+  if (kv)
+    ADEPT_TRY(check_paged_step("layer_step_quant", a, kv, page_table, max_pages, cache_slot));
   const PagedStep pg{kv, page_table, max_pages, cache_slot};
   return layer_step(a, layer, kv ? &pg : nullptr, w, stream);
 }
-
 
 namespace adept {
 namespace {

@@ -1,5 +1,6 @@
 """Sizes that a call over 4-bit weights does not take: refused before anything is launched, and
 what a model does with a pass of that many rows."""
+import ctypes
 from types import SimpleNamespace
 
 import pytest
@@ -8,6 +9,7 @@ import torch
 import adept_inputs as ai
 from paper_2601_03700_amd import binding as B
 from paper_2601_03700_amd.model import DecoderModel
+from tests import test_serving_refusals as R
 
 A = 1 << 20          # an aligned address that is never read
 
@@ -64,3 +66,22 @@ def test_a_head_that_no_call_takes_whole_is_split(monkeypatch, nr):
     for r, x, y in calls:
         assert (x, y) == (at * D, at * V)
         at += len(r)
+
+
+FP8 = dict(dtype=B.KV_FP8, k_scale=A, v_scale=A, n_kv_heads=4)
+
+
+@pytest.mark.parametrize("a,c,table,pages,slot", [
+    (dict(), dict(n_kv_heads=2), A, 4, None), (dict(), dict(n_kv_heads=4, page_size=3), A, 4, None),
+    (dict(n_seq=0), dict(n_kv_heads=4), A, 4, None), (dict(), dict(n_kv_heads=4), None, 4, None),
+    (dict(), dict(n_kv_heads=4), A, 4, None), (dict(), FP8, A, 4, None), (dict(n_slots=7), FP8, A, 4, A),
+    (dict(k_cache=A + 2), FP8, A, 4, A), (dict(kv_fused=0, attn_tiles=0), FP8, A, 4, A)], ids=str)
+def test_errors_of_paged_steps_name_the_call(a, c, table, pages, slot):
+    args, cache = R.layer_args(**a), R.kv(**c)
+    kv = ctypes.byref(cache)
+    assert B.lib().adept_layer_step_quant(ctypes.byref(args), ctypes.byref(R.layer_weights()), kv, table,
+                                          pages, slot, 1, None) == -1
+    of_quant = B.lib().adept_last_error()
+    assert of_quant.startswith(b"layer_step_quant: ")
+    assert B.lib().adept_layer_step_paged(ctypes.byref(args), kv, table, pages, slot, 1, None) == -1
+    assert B.lib().adept_last_error() == of_quant.replace(b"step_quant", b"step_paged")
