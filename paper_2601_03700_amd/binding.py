@@ -623,6 +623,14 @@ class QuantWeights:
     [n_mats, bytes]."""
 
     def __init__(self, n, k, codes, scales):
+        # (the kernels go by n and k)
+        for t, size in ((codes, lib().adept_quant_codes_bytes(n, k)),
+                        (scales, lib().adept_quant_scales_bytes(n, k))):
+            _need(size > 0 and t.dtype is torch.uint8 and t.dim() == 2 and t.shape[0] >= 1 and
+                  t.shape[1] == size and t.is_contiguous(), "quant_weights",
+                  f"matrices of {n} x {k} are contiguous uint8 [n_mats, {size}]")
+        _need(codes.shape[0] == scales.shape[0] and codes.device == scales.device, "quant_weights",
+              "codes and scales of as many matrices, on one device")
         self.n, self.k, self.codes, self.scales = n, k, codes, scales
 
     @property
