@@ -643,13 +643,16 @@ adept_status dir_rows(const GP& p, const RowList& rl, int row_norm, const char* 
 // an estimate of a CU's time, from its share of the workgroups: what their waves do a
 // piece (the activations' part grows with the rows, the weights' with NB), their fixed
 // part, and the rounds of pieces that wait for each other, of up to 16 waves at a time.
-// The weights of the four are fitted to the times of 315 shapes (1 to 64 rows, n 320 ..
-// 50304, k 512 .. 11008) in all of NB = 1, 2, 4 and W = 4, 8, 16: the choice is 1.5 %
-// behind the best on average and 11 % at most.  No form serves all: 16 rows of
-// 4096 x 11008 11.0 us with 1 x 16 and 16.0 with 4 x 16, 64 rows of 11008 x 4096 16.0
-// with 4 x 4 and 21.2 with 2 x 8, 1 row of 22016 x 4096 11.9 with 2 x 4 and 15.8 with
-// 1 x 4.  More activation rows of a workgroup (32, 64) convert the weights less often,
-// but few of them fit a CU: 64 rows of 11008 x 4096 18.6 us.
+// The weights of the four were fitted to the times of 315 shapes (1 to 64 rows, n 320 ..
+// 50304, k 512 .. 11008) before the loads had scalar addresses.  Of the kernel as it is,
+// over the same shapes in all of NB = 1, 2, 4 and W = 4, 8, 16, the choice is 0.3 %
+// behind the best of these five on average and 11 % at most, and 1.5 % and 17 % behind
+// the best of all nine (64 rows of 8192 x 11008: 27.4 us with 4 x 4, 23.3 with 4 x 8).
+// No form serves all, in graphs of 24 launches: 16 rows of 4096 x 11008 10.2 us with
+// 1 x 16 and 15.1 with 4 x 16, 64 rows of 11008 x 4096 15.6 with 4 x 4 and 20.5 with
+// 2 x 8, 1 row of 22016 x 4096 11.6 with 2 x 4 and 15.2 with 1 x 4.  More activation
+// rows of a workgroup (32, 64) convert the weights less often, but few of them fit a
+// CU: 64 rows of 11008 x 4096 18.6 us, where one block of them took 16.0.
 struct QuantForm { int nb, w; };
 QuantForm quant_form(int rows, int n_weights, int K) {
   static const QuantForm forms[] = {{1, 16}, {2, 16}, {2, 8}, {2, 4}, {4, 4}};

@@ -8,17 +8,17 @@
 // A token is the border between two sums, so everything behind the logits is in 64
 // bits: a weight exp((l - max) / T), the sums, the comparisons.  With sums off by 1e-7,
 // as in 32 bits, one draw in some hundred from a flat row of 32000 tokens (3e-5 each)
-// would come from the other side of its border.  The vector units take 64-bit products and sums at the rate of unpacked
-// 32-bit ones, and one exponential is about 20 of them.
+// would come from the other side of its border.  The vector units take 64-bit products
+// and sums at the rate of unpacked 32-bit ones, and one exponential is about 20 of them.
 //
 // Two kernels.  The first takes the maximum and the sum of every row, 1024 logits a
 // wave: all of the traffic, each logit once.  The second has a few workgroups for each
 // sequence: every one makes the decision for itself (some partial sums from L2, less
 // than one more kernel costs), takes its share of what p - q holds, and the last of them
 // draws the token, by the shares' sums and then inside one.  64 sequences x 8 drafts x
-// 32000 logits, f32: 31 and 18.5 us (4.1 TB/s, and 73 % of the SIMDs' cycles for the
-// exponentials, in the first; round trips to memory in the second), one sequence x 4:
-// 3.5 and 11.
+// 32000 logits, f32: 33 and 20 us (at best 31 and 18.5: 4.1 TB/s, and 73 % of the SIMDs'
+// cycles for the exponentials, in the first; round trips to memory in the second), one
+// sequence x 4: 3.8 and 11.7.
 #include <algorithm>
 #include <climits>
 

@@ -698,9 +698,9 @@ class DecoderModel:
         [n, g] behind it, and their verification: (tokens [n, g+1], kept [n], pass result).  The
         cache then holds the last token and the drafts; those that were not kept are written
         over by what comes next.  It stands for decode passes: every token decides for itself
-        when it exits, also where cfg lets a prompt's last token decide.  draft_logits [n, g, V] f32 (None: the drafts have no
-        probabilities); u [n, g+1]; temperature [n]; pos_max: the largest pos, when known on the
-        host."""
+        when it exits, also where cfg lets a prompt's last token decide.  draft_logits [n, g, V]
+        f32 (None: the drafts have no probabilities); u [n, g+1]; temperature [n]; pos_max: the
+        largest pos, when known on the host."""
         n, g = drafts.shape
         self._check_sequences(cache, n)
         top = pos_max if pos_max is not None else (int(pos.max()) if n else 0)
@@ -739,7 +739,7 @@ class DecoderModel:
         temp = torch.full((n,), float(temperature), dtype=torch.float32, device=dev)
         rand = lambda *d: torch.rand(d, generator=generator, device=dev)
         res, _ = self.prefill(ids_t, cfg, logits="last", cache=cache)
-        # out[:, n_steps] takes what a finished sequence still draws
+        # the last column takes what a finished sequence still draws, and what was not kept
         out = torch.zeros((n, n_steps + n_draft + 1), **i32)
         out[:, 0] = self.draw(res.logits, rand(n), temp)
         have = torch.ones(n, **i32)         # tokens of each sequence
