@@ -751,19 +751,27 @@ def _paged_step(what, args, kv, page_table, cache_slot):
     return _i32_ptrs(what, _device_of(what, kv), page_table, cache_slot)
 
 
+def _layer_sizes(args):
+    return args.d_model, args.n_heads * args.head_dim, args.d_ff, args.family
+
+
 def quant_layers(args: LayerArgs, qkv, o, gate, up, down):
     """Descriptor of the layers' weights in 4 bits (QuantWeights of all layers each; up None in the
     GPT2 family), which it holds."""
-    N, D, dq, F = args.n_layers, args.d_model, args.n_heads * args.head_dim, args.d_ff
+    N = args.n_layers
+    D, dq, F, family = _layer_sizes(args)
     q = QuantLayers()
+    q.weights, q.sizes, q.layers = (qkv, o, gate, up, down), (D, dq, F, family), None
     for name, w, n, k in (("qkv", qkv, 3 * dq, D), ("o", o, D, dq), ("gate", gate, F, D),
                           ("up", up, F, D), ("down", down, D, F)):
-        if w is None and name == "up" and args.family == FAMILY_GPT2:
+        if w is None and name == "up" and family == FAMILY_GPT2:
             continue
         if w is None or (w.n, w.k) != (n, k) or w.n_mats < N:
             raise AdeptError(f"quant_layers: {name} must be {N} matrices of {n} x {k}")
+        if w.codes.device != qkv.codes.device:
+            raise AdeptError("quant_layers: weights on one device")
+        q.layers = w.n_mats if q.layers is None else min(q.layers, w.n_mats)
         setattr(q, name, QuantMat(w.codes.data_ptr(), w.scales.data_ptr()))
-    q.weights = (qkv, o, gate, up, down)
     return q
 
 
@@ -776,6 +784,13 @@ def layer_quant_workspace_bytes(args: LayerArgs, weights, kv=None, max_pages=0):
 def layer_step_quant(args: LayerArgs, weights, layer, kv=None, page_table=None, cache_slot=None,
                      stream=None):
     """layer_step (kv None) or layer_step_paged with the weights in 4 bits as well (quant_layers)."""
+    if args.n_layers > weights.layers or _layer_sizes(args) != weights.sizes:
+        raise AdeptError(f"layer_step_quant: weights of {weights.layers} layers, width, H*hd, d_ff and "
+                         f"family {weights.sizes}; the arguments have {args.n_layers}, "
+                         f"{_layer_sizes(args)}")
+    dev = weights.weights[0].codes.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise _elsewhere("layer_step_quant")
     tp = cp = None
     if kv is not None:
         tp, cp = _paged_step("layer_step_quant", args, kv, page_table, cache_slot)
